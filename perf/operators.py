@@ -329,7 +329,7 @@ def _plain_table(s):
     back = torch.where(gone, have, 0)
     cu, pu, bu = ((torch.cat([x.new_zeros(1), x.cumsum(0)])) for x in (more, need, back))
     status = torch.stack([(pu[-1] - count).clamp(min=0), (have + need > W).sum(), (cu[-1] - cap).clamp(min=0),
-                          (count - pu[-1] + bu[-1] - pages).clamp(min=0)])
+                          (count + bu[-1] - pages).clamp(min=0)])
     ok = (status == 0).all()
     lens = torch.where(ok, torch.where(gone, 0, past + more), past)
     state = torch.where(ok, torch.stack([(head + pu[-1]) % pages, count - pu[-1] + bu[-1]]), s["ring_state"].long())
