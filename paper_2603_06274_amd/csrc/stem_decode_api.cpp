@@ -1,0 +1,288 @@
+// Host side of include/stem_decode.h: argument checks, rotary frequencies, workspace layouts and the split of the attention
+// to a shared prefix.  No allocation, no synchronisation.
+#include <cmath>
+#include <limits>
+
+#include "stem_decode_common.h"
+
+namespace stem {
+
+constexpr int64_t kInt32Max = 0x7fffffff;
+
+static bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Strides of [tokens, heads, head_dim] rows.
+static bool good_strides(int64_t token, int64_t head, int32_t head_dim) {
+    return token >= head_dim && head >= head_dim && !((token | head) & 7);
+}
+
+static int check_page_size(int32_t n) {
+    if (n <= 0) return STEM_ERR_INVALID_ARG;
+    return n == 16 || n == 32 || n == 64 || n == 128 || n == 256 ? STEM_OK : STEM_ERR_UNSUPPORTED;
+}
+
+static int check_pages(const stem_pages& p, int32_t head_dim) {
+    if (const int st = check_page_size(p.page_size)) return st;
+    if (p.num_pages < 0) return STEM_ERR_INVALID_ARG;
+    if ((int64_t)p.num_pages * p.page_size > kInt32Max) return STEM_ERR_UNSUPPORTED;
+    if (!good_strides(p.stride_token, p.stride_head, head_dim) || p.stride_page < head_dim || (p.stride_page & 7))
+        return STEM_ERR_INVALID_ARG;
+    return STEM_OK;
+}
+
+static int check_rotary(const stem_rotary_shape* s, const void* q, const void* k, const int32_t* positions,
+                        const double* turns, float factor, const void* q_out) {
+    if (!s) return STEM_ERR_INVALID_ARG;
+    if (s->dtype != STEM_BF16 && s->dtype != STEM_FP16 && s->dtype != STEM_FP32) return STEM_ERR_INVALID_ARG;
+    if (s->tokens < 0 || s->num_q_heads < 0 || s->num_kv_heads < 0) return STEM_ERR_INVALID_ARG;
+    if (s->tokens > 1 << 24 || (int64_t)s->num_q_heads + 2 * (int64_t)s->num_kv_heads > 65535) return STEM_ERR_UNSUPPORTED;
+    if (s->num_q_heads + s->num_kv_heads == 0 || s->head_dim <= 0 || s->head_dim % 8) return STEM_ERR_INVALID_ARG;
+    if (s->head_dim > STEM_MAX_HEAD_DIM) return STEM_ERR_UNSUPPORTED;
+    if (s->rotary_dim < 2 || s->rotary_dim % 2 || s->rotary_dim > s->head_dim) return STEM_ERR_INVALID_ARG;
+    if (s->layout != STEM_ROTARY_HALF && s->layout != STEM_ROTARY_INTERLEAVED) return STEM_ERR_INVALID_ARG;
+    if (!std::isfinite(factor)) return STEM_ERR_INVALID_ARG;
+    if (!positions || !aligned(positions, 4) || !turns || !aligned(turns, 8)) return STEM_ERR_INVALID_ARG;
+    if (s->num_q_heads > 0) {
+        if (!q || !aligned(q, 16) || !q_out || !aligned(q_out, 16)) return STEM_ERR_INVALID_ARG;
+        if (!good_strides(s->q_stride_token, s->q_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
+        if (!good_strides(s->q_out_stride_token, s->q_out_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
+        if (q == q_out && (s->q_stride_token != s->q_out_stride_token || s->q_stride_head != s->q_out_stride_head))
+            return STEM_ERR_INVALID_ARG;
+    }
+    if (s->num_kv_heads > 0) {
+        if (!k || !aligned(k, 16)) return STEM_ERR_INVALID_ARG;
+        if (!good_strides(s->k_stride_token, s->k_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
+    }
+    return STEM_OK;
+}
+
+TableWorkspace table_workspace(int32_t requests) {
+    TableWorkspace w;
+    w.pages_before = 0;
+    w.back_before = align256(sizeof(int32_t) * (size_t)requests);
+    w.ring = w.back_before + align256(sizeof(int32_t) * (size_t)requests);
+    w.total = w.ring + 256;
+    return w;
+}
+
+static int check_table(const stem_table_shape* s) {
+    if (!s) return STEM_ERR_INVALID_ARG;
+    if (s->requests < 1 || s->num_pages < 1 || s->pages_per_request < 1 || s->token_capacity < 0 || s->position_offset < 0)
+        return STEM_ERR_INVALID_ARG;
+    if (const int st = check_page_size(s->page_size)) return st;
+    if (s->requests > STEM_MAX_REQUESTS) return STEM_ERR_UNSUPPORTED;
+    if ((int64_t)s->requests * s->pages_per_request > kInt32Max || (int64_t)s->num_pages * s->page_size > kInt32Max ||
+        s->position_offset + (int64_t)s->pages_per_request * s->page_size > kInt32Max)
+        return STEM_ERR_UNSUPPORTED;
+    return STEM_OK;
+}
+
+static int check_prefix(const stem_prefix_shape* s) {
+    if (!s) return STEM_ERR_INVALID_ARG;
+    if (s->dtype != STEM_BF16 && s->dtype != STEM_FP16) return STEM_ERR_INVALID_ARG;
+    if (s->num_q_heads <= 0 || s->num_kv_heads <= 0 || s->num_q_heads % s->num_kv_heads) return STEM_ERR_INVALID_ARG;
+    if (s->head_dim <= 0 || s->requests < 1 || s->tokens < 0 || s->max_new < 1 || s->prefix_len < 0 || s->max_suffix < 0)
+        return STEM_ERR_INVALID_ARG;
+    if (s->head_dim != 64 && s->head_dim != 128 && s->head_dim != 256) return STEM_ERR_UNSUPPORTED;
+    if (s->requests > STEM_MAX_REQUESTS || s->num_q_heads > 65535) return STEM_ERR_UNSUPPORTED;
+    // rows are counted in 32 bits
+    if ((int64_t)s->tokens * s->num_q_heads > kInt32Max || (int64_t)s->max_new * s->num_q_heads > kInt32Max)
+        return STEM_ERR_UNSUPPORTED;
+    if (!good_strides(s->q_stride_token, s->q_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
+    // the kernel addresses 16 rows through a 32-bit byte offset
+    const int64_t most = (kInt32Max - 2 * s->head_dim) / (2 * 15);
+    if (s->prefix_len > 0) {
+        if (!good_strides(s->prefix_stride_token, s->prefix_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
+        if (s->prefix_stride_token > most) return STEM_ERR_UNSUPPORTED;
+    }
+    if (s->max_suffix > 0) {
+        if (const int st = check_pages(s->pages, s->head_dim)) return st;
+        if (s->pages.stride_token > most) return STEM_ERR_UNSUPPORTED;
+        if (s->pages_per_request < 1) return STEM_ERR_INVALID_ARG;
+        if ((int64_t)s->pages_per_request * s->pages.page_size < s->max_suffix) return STEM_ERR_INVALID_ARG;
+        if ((int64_t)s->requests * s->pages_per_request > kInt32Max) return STEM_ERR_UNSUPPORTED;
+    }
+    return STEM_OK;
+}
+
+int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
+    const int cus = units();
+    if (cus <= 0) return STEM_ERR_HIP;
+    const int64_t G = s.num_q_heads / s.num_kv_heads, rows = s.tokens * G;
+    const int32_t most = s.head_dim == 256 ? 32 : 64;
+    PrefixPlan p;
+    p.row_tile = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : most;
+    p.row_tiles = (int32_t)((rows + p.row_tile - 1) / p.row_tile);
+    p.prefix_splits = p.split_keys = 0;
+    if (s.prefix_len > 0 && rows > 0) {
+        const int64_t others = (int64_t)p.row_tiles * s.num_kv_heads;
+        const int64_t wanted = (cus + others - 1) / others;
+        const int64_t tiles = (s.prefix_len + 127) / 128;
+        const int64_t splits = wanted < tiles ? wanted : tiles;
+        const int64_t each = (tiles + splits - 1) / splits;
+        p.split_keys = (int32_t)(each * 128);
+        p.prefix_splits = (int32_t)((tiles + each - 1) / each);
+    }
+    const int64_t own_rows = s.max_new * G;
+    p.suffix_row_tile = own_rows <= 16 ? 16 : p.row_tile;
+    p.suffix_row_tiles = (int32_t)((own_rows + p.suffix_row_tile - 1) / p.suffix_row_tile);
+    p.suffix_splits = 0;
+    if (s.max_suffix > 0 && rows > 0) {
+        const int64_t others = (int64_t)s.requests * s.num_kv_heads * p.suffix_row_tiles;
+        const int64_t wanted = (2 * (int64_t)cus + others - 1) / others;
+        const int64_t tiles = (s.max_suffix + 255) / 256;
+        p.suffix_splits = (int32_t)(wanted < tiles ? wanted : tiles);
+        if (p.suffix_splits > 64) p.suffix_splits = 64;
+    }
+    const int64_t parts = (int64_t)(p.prefix_splits + p.suffix_splits) * s.num_kv_heads * rows;
+    p.partial_ml = align256(sizeof(float) * (size_t)parts * s.head_dim);
+    p.bytes = p.partial_ml + align256(2 * sizeof(float) * (size_t)parts);
+    if (p.bytes == 0) p.bytes = 256;
+    *plan = p;
+    return STEM_OK;
+}
+
+}  // namespace stem
+
+using namespace stem;
+
+extern "C" {
+
+int stem_rotary_frequencies(int32_t rotary_dim, double theta, const stem_rotary_scaling* scaling, double* host_turns,
+                            double* host_attention_factor) {
+    if (rotary_dim < 2 || rotary_dim % 2 || !host_turns || !host_attention_factor) return STEM_ERR_INVALID_ARG;
+    if (rotary_dim > STEM_MAX_HEAD_DIM) return STEM_ERR_UNSUPPORTED;
+    if (!std::isfinite(theta) || !(theta > 1.0)) return STEM_ERR_INVALID_ARG;
+    const int32_t kind = scaling ? scaling->kind : STEM_ROTARY_NONE;
+    if (kind < STEM_ROTARY_NONE || kind > STEM_ROTARY_BANDS) return STEM_ERR_INVALID_ARG;
+    const double r = rotary_dim, two_pi = 6.283185307179586;
+    double factor = 1.0, trained = 0.0, low = 0.0, high = 0.0;
+    if (kind != STEM_ROTARY_NONE) {
+        factor = scaling->factor;
+        if (!std::isfinite(factor) || !(factor >= 1.0)) return STEM_ERR_INVALID_ARG;
+    }
+    if (kind == STEM_ROTARY_NTK) {
+        if (rotary_dim == 2) return STEM_ERR_INVALID_ARG;
+        theta *= std::pow(factor, r / (r - 2.0));
+        if (!std::isfinite(theta)) return STEM_ERR_INVALID_ARG;
+    }
+    double ramp_lo = 0.0, ramp_span = 1.0;
+    if (kind == STEM_ROTARY_YARN || kind == STEM_ROTARY_BANDS) {
+        trained = scaling->trained_length;
+        low = scaling->low;
+        high = scaling->high;
+        if (!std::isfinite(trained) || !(trained > 0.0) || !std::isfinite(low) || !std::isfinite(high) || !(low > 0.0) ||
+            !(high > low))
+            return STEM_ERR_INVALID_ARG;
+        auto dim = [&](double n) { return r * std::log(trained / (n * two_pi)) / (2.0 * std::log(theta)); };
+        if (kind == STEM_ROTARY_YARN) {
+            ramp_lo = std::fmax(std::floor(dim(high)), 0.0);
+            ramp_span = std::fmax(std::fmin(std::ceil(dim(low)), r - 1.0) - ramp_lo, 0.001);
+        }
+    }
+    for (int32_t i = 0; i < rotary_dim / 2; ++i) {
+        const double f = std::pow(theta, -2.0 * i / r);
+        double share = 0.0;                            // of f / factor
+        if (kind == STEM_ROTARY_LINEAR) share = 1.0;
+        else if (kind == STEM_ROTARY_YARN) share = std::fmin(std::fmax((i - ramp_lo) / ramp_span, 0.0), 1.0);
+        else if (kind == STEM_ROTARY_BANDS)
+            share = 1.0 - std::fmin(std::fmax((trained * f / two_pi - low) / (high - low), 0.0), 1.0);
+        host_turns[i] = (f * (1.0 - share) + f / factor * share) / two_pi;
+    }
+    *host_attention_factor = kind == STEM_ROTARY_YARN ? 0.1 * std::log(factor) + 1.0 : 1.0;
+    return STEM_OK;
+}
+
+int stem_rotary(const stem_rotary_shape* shape, const void* q, const void* k, const int32_t* positions,
+                const double* turns, float attention_factor, int32_t backward, void* q_out, void* k_out,
+                void* hip_stream) {
+    if (const int st = check_rotary(shape, q, k, positions, turns, attention_factor, q_out)) return st;
+    if (backward != 0 && backward != 1) return STEM_ERR_INVALID_ARG;
+    const stem_rotary_shape& s = *shape;
+    if (s.num_kv_heads > 0) {
+        if (!k_out || !aligned(k_out, 16)) return STEM_ERR_INVALID_ARG;
+        if (!good_strides(s.k_out_stride_token, s.k_out_stride_head, s.head_dim)) return STEM_ERR_INVALID_ARG;
+        if (k == k_out && (s.k_stride_token != s.k_out_stride_token || s.k_stride_head != s.k_out_stride_head))
+            return STEM_ERR_INVALID_ARG;
+    }
+    if (s.tokens == 0) return STEM_OK;
+    const RotaryCall call = {s, q, k, nullptr, q_out, k_out, nullptr, positions, nullptr, turns, attention_factor, backward, {}};
+    return launch_rotary(call, static_cast<hipStream_t>(hip_stream));
+}
+
+int stem_rotary_append(const stem_rotary_shape* shape, const stem_pages* pages, const void* q, const void* k,
+                       const void* v, const int32_t* positions, const int32_t* slots, const double* turns,
+                       float attention_factor, void* q_out, void* k_pages, void* v_pages, void* hip_stream) {
+    if (const int st = check_rotary(shape, q, k, positions, turns, attention_factor, q_out)) return st;
+    const stem_rotary_shape& s = *shape;
+    if (!pages || s.num_kv_heads == 0) return STEM_ERR_INVALID_ARG;
+    if (const int st = check_pages(*pages, s.head_dim)) return st;
+    if (!slots || !aligned(slots, 4) || !v || !aligned(v, 16)) return STEM_ERR_INVALID_ARG;
+    if (!k_pages || !aligned(k_pages, 16) || !v_pages || !aligned(v_pages, 16)) return STEM_ERR_INVALID_ARG;
+    if (s.tokens == 0 || pages->num_pages == 0) return STEM_OK;
+    const RotaryCall call = {s, q, k, v, q_out, k_pages, v_pages, positions, slots, turns, attention_factor, 0, *pages};
+    return launch_rotary(call, static_cast<hipStream_t>(hip_stream));
+}
+
+int stem_block_table_workspace_bytes(const stem_table_shape* shape, size_t* host_bytes) {
+    if (const int st = check_table(shape)) return st;
+    if (!host_bytes) return STEM_ERR_INVALID_ARG;
+    *host_bytes = table_workspace(shape->requests).total;
+    return STEM_OK;
+}
+
+int stem_block_table(const stem_table_shape* shape, const int32_t* past_lens, const int32_t* new_lens,
+                     const int32_t* ring_state, int32_t* ring, int32_t* table, int32_t* lens, int32_t* ring_state_out,
+                     int32_t* cu_new, int32_t* positions, int32_t* slots, int32_t* status, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+    if (const int st = check_table(shape)) return st;
+    const void* needed[] = {past_lens, ring_state, ring, table, lens, ring_state_out, cu_new, status};
+    for (const void* p : needed)
+        if (!p || !aligned(p, 4)) return STEM_ERR_INVALID_ARG;
+    if (!aligned(new_lens, 4) || !aligned(positions, 4) || !aligned(slots, 4)) return STEM_ERR_INVALID_ARG;
+    if (shape->token_capacity > 0 && (!positions || !slots)) return STEM_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16)) return STEM_ERR_INVALID_ARG;
+    const TableWorkspace w = table_workspace(shape->requests);
+    if (workspace_bytes < w.total) return STEM_ERR_WORKSPACE;
+    char* ws = static_cast<char*>(workspace);
+    auto part = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
+    const TableCall call = {*shape, past_lens, new_lens, ring_state, ring, table, lens, ring_state_out, cu_new, positions, slots, status,
+                            part(w.pages_before), part(w.back_before), part(w.ring)};
+    return launch_block_table(call, static_cast<hipStream_t>(hip_stream));
+}
+
+int stem_prefix_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* host_bytes) {
+    if (const int st = check_prefix(shape)) return st;
+    if (!host_bytes) return STEM_ERR_INVALID_ARG;
+    PrefixPlan plan;
+    if (const int st = prefix_plan(*shape, &plan)) return st;
+    *host_bytes = plan.bytes;
+    return STEM_OK;
+}
+
+int stem_prefix_attn(const stem_prefix_shape* shape, const void* q, const void* prefix_k, const void* prefix_v,
+                     const void* k_pages, const void* v_pages, const int32_t* table, const int32_t* lens,
+                     const int32_t* cu_new, float softmax_scale, void* out, float* lse, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+    if (const int st = check_prefix(shape)) return st;
+    const stem_prefix_shape& s = *shape;
+    if (!q || !aligned(q, 16) || !out || !aligned(out, 16) || q == out || !aligned(lse, 4)) return STEM_ERR_INVALID_ARG;
+    if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.f)) return STEM_ERR_INVALID_ARG;
+    if (s.prefix_len > 0 && (!prefix_k || !aligned(prefix_k, 16) || !prefix_v || !aligned(prefix_v, 16)))
+        return STEM_ERR_INVALID_ARG;
+    if (s.max_suffix > 0) {
+        if (!table || !aligned(table, 4) || !lens || !aligned(lens, 4)) return STEM_ERR_INVALID_ARG;
+        if (s.pages.num_pages > 0 && (!k_pages || !aligned(k_pages, 16) || !v_pages || !aligned(v_pages, 16)))
+            return STEM_ERR_INVALID_ARG;
+    }
+    if (!aligned(cu_new, 4) || (!cu_new && s.tokens != s.requests)) return STEM_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16)) return STEM_ERR_INVALID_ARG;
+    if (s.tokens == 0) return STEM_OK;
+    PrefixCall call = {s, {}, q, prefix_k, prefix_v, k_pages, v_pages, table, lens, cu_new, softmax_scale, out, lse, workspace};
+    if (const int st = prefix_plan(s, &call.plan)) return st;
+    if (workspace_bytes < call.plan.bytes) return STEM_ERR_WORKSPACE;
+    return launch_prefix_attn(call, static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,76 @@
+// Internal declarations shared by the host API (stem_decode_api.cpp) and the kernels of include/stem_decode.h.
+#pragma once
+
+#include "stem_common.h"
+#include "stem_decode.h"
+
+namespace stem {
+
+// --- rotary positions ---------------------------------------------------------------------------------------
+
+struct RotaryCall {
+    stem_rotary_shape shape;
+    const void *q, *k, *v;
+    void *q_out, *k_out, *v_out;         // k_out and v_out: the pages, if `pages` says so
+    const int32_t* positions;
+    const int32_t* slots;                // nullptr: no pages
+    const double* turns;
+    float factor;
+    int32_t backward;
+    stem_pages pages;
+};
+int launch_rotary(const RotaryCall& call, hipStream_t stream);
+
+// --- block tables -------------------------------------------------------------------------------------------
+
+// What the first of two launches leaves for the second: sums over the requests before each, and the ring's state.
+struct TableWorkspace {
+    size_t pages_before, back_before, ring, total;
+};
+TableWorkspace table_workspace(int32_t requests);
+
+struct TableCall {
+    stem_table_shape shape;
+    const int32_t *past_lens, *new_lens, *ring_state;
+    int32_t *ring, *table, *lens, *ring_state_out, *cu_new, *positions, *slots, *status;
+    int32_t *pages_before, *back_before, *ring_then;   // workspace
+};
+int launch_block_table(const TableCall& call, hipStream_t stream);
+
+// --- attention to a shared prefix ---------------------------------------------------------------------------
+
+// How a call is split over workgroups.  Rows are (token, query head of the group) per KV head.
+struct PrefixPlan {
+    int32_t row_tile;          // rows of a workgroup in the prefix, and per request in its pages
+    int32_t row_tiles;         // of the prefix: ceil(tokens * G / row_tile)
+    int32_t prefix_splits;     // 0 if there is no prefix
+    int32_t split_keys;        // keys per split (a multiple of 32), the last may be shorter
+    int32_t suffix_row_tile;
+    int32_t suffix_row_tiles;  // per request: ceil(max_new * G / suffix_row_tile)
+    int32_t suffix_splits;     // 0 if there are no pages
+    size_t partial_ml;         // byte offset in the workspace: (maximum, sum) of every partial result
+    size_t bytes;
+};
+// units: where the number of compute units comes from
+int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)() = compute_units);
+
+struct PrefixCall {
+    stem_prefix_shape shape;
+    PrefixPlan plan;
+    const void *q, *prefix_k, *prefix_v, *k_pages, *v_pages;
+    const int32_t *table, *lens, *cu_new;
+    float softmax_scale;
+    void* out;
+    float* lse;
+    void* workspace;
+};
+int launch_prefix_attn(const PrefixCall& call, hipStream_t stream);
+
+// Keys per request split of `suffix_splits`: whole tiles of 32, at least `least` of them, so that short suffixes use few
+// splits.  The kernel that computes partial results and the one that joins them both ask here.
+__host__ __device__ inline int suffix_split_tiles(int tiles, int splits, int least) {
+    const int each = (tiles + splits - 1) / splits;
+    return each > least ? each : least;
+}
+
+}  // namespace stem
