@@ -173,8 +173,8 @@ int stem_prefix_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* hos
  * over the prefix_len rows of prefix_k, prefix_v [prefix_len, Hkv, d] and the request's rows j in the pages with
  * j <= lens[r] - n + i, where t is number i of the n new tokens of request r (which stand at the end of its lens[r] tokens).
  *   - lens is int32 [requests], table int32 [requests, pages_per_request], cu_new int32 [requests + 1]: request r's new tokens are
- *     the rows cu_new[r] .. cu_new[r + 1] - 1 of Q and O (none if that is negative).  cu_new NULL: one token each, then
- *     tokens = requests.  Rows of no request are left as they were, in O and in lse, and so are a request's rows from max_new on.
+ *     the rows cu_new[r] .. cu_new[r + 1] - 1 of Q and O, as far as there are such rows (none if there are none between; a row that a
+ *     cu_new which descends gives to two requests holds nothing defined).  cu_new NULL: one token each, then tokens = requests.  Rows of no request are left as they were, in O and in lse, and so are a request's rows from max_new on.
  *   - lens outside 0 .. max_suffix count as the nearer of the two.  Rows in pages that are not the cache's (a table entry outside
  *     0 .. num_pages - 1) contribute nothing, and nothing is read there; nor is anything behind a request's last token.
  *   - A row that sees no key at all gives zeros, lse -inf.
