@@ -32,7 +32,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-I" + os.path.
 # control-flow structurizing they stay plain branches.  Structurized, the value of every register that such a branch may change
 # was copied on the common path too, and the B = 128, d = 128 kernel spilled 79 registers.  Results of the matrix instructions
 # that the compiler places stay in vector registers also in a kernel that uses accumulator registers by hand (head size 256).
-FLAGS = {"stem_attn.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions", "-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FLAGS = {"stem_attn.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions", "-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "stem_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc() -> str:

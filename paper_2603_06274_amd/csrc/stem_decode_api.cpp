@@ -110,9 +110,9 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     const int cus = units();
     if (cus <= 0) return STEM_ERR_HIP;
     const int64_t G = s.num_q_heads / s.num_kv_heads, rows = s.tokens * G;
-    const int32_t most = s.head_dim == 256 ? 32 : 64;
     PrefixPlan p;
-    p.row_tile = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : most;
+    auto tile_of = [](int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; };
+    p.row_tile = tile_of(rows);
     p.row_tiles = (int32_t)((rows + p.row_tile - 1) / p.row_tile);
     p.prefix_splits = p.split_keys = 0;
     if (s.prefix_len > 0 && rows > 0) {
@@ -124,8 +124,8 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
         p.split_keys = (int32_t)(each * 128);
         p.prefix_splits = (int32_t)((tiles + each - 1) / each);
     }
-    const int64_t own_rows = s.max_new * G;
-    p.suffix_row_tile = own_rows <= 16 ? 16 : p.row_tile;
+    const int64_t own_rows = s.max_new * G < rows ? s.max_new * G : rows;
+    p.suffix_row_tile = own_rows <= 16 ? 16 : 64;
     p.suffix_row_tiles = (int32_t)((own_rows + p.suffix_row_tile - 1) / p.suffix_row_tile);
     p.suffix_splits = 0;
     if (s.max_suffix > 0 && rows > 0) {

@@ -66,11 +66,11 @@ struct PrefixCall {
 };
 int launch_prefix_attn(const PrefixCall& call, hipStream_t stream);
 
-// Keys per request split of `suffix_splits`: whole tiles of 32, at least `least` of them, so that short suffixes use few
-// splits.  The kernel that computes partial results and the one that joins them both ask here.
-__host__ __device__ inline int suffix_split_tiles(int tiles, int splits, int least) {
-    const int each = (tiles + splits - 1) / splits;
-    return each > least ? each : least;
+// Keys of a part of a request's own `len`, of which there are at most `splits`: whole 128s, so that short ones use few parts.  The
+// kernel that computes partial results and the one that joins them both ask here.
+__host__ __device__ inline int suffix_split_keys(int len, int splits) {
+    const int each = (int)(((int64_t)len + splits - 1) / splits);
+    return (each + 127) & ~127;
 }
 
 }  // namespace stem

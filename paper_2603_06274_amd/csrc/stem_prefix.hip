@@ -7,14 +7,14 @@
 // joins them (join_kernel).  The prefix is one dense product of all requests' rows together, so K and V of the prefix are read once
 // for all of them; the keys are split so that every CU has a part.
 //
-// A workgroup's waves share the rows and take turns over tiles of 32 keys, each wave with tiles, softmax and o of its own, joined at its
-// end through LDS: no barrier while keys go by.  Products and softmax are those of stage 3: S^T = K Q^T, so that one query is one lane's
-// column and its softmax needs no exchange but at its start and when its reference moves; P^T lies in the registers as the second
-// product O^T += V^T P^T takes it, V^T comes from row-major V by transposing LDS reads.
+// Products and softmax are those of stage 3: S^T = K Q^T, so that one query is one lane's column and its softmax needs no exchange
+// but when its reference moves and at the end; P^T lies in the registers as the second product O^T += V^T P^T takes it, V^T comes from
+// row-major V by transposing LDS reads.  Every wave has a softmax and an o of its own; those over other keys of the same rows are
+// joined at a workgroup's end through LDS.
 //
-// K and V go from global memory straight into LDS (one tile ahead), 16 keys per buffer resource: its size ends with the last valid
-// row, so that rows behind it, and all of a page that is none, arrive as zeros and are masked.  A tile of 32 keys begins at a multiple
-// of 32, so each of its halves lies in one page.
+// K and V are on their way to registers for one tile while the tile before is used from LDS.  Rows are asked for by up to 16, through a
+// buffer resource whose size ends with the last valid one: rows behind it, and all of a page that is none, arrive as zeros and
+// are masked.  A tile begins at a multiple of 16 keys, so 16 rows lie in one page.
 #include <type_traits>
 
 #include "stem_decode_common.h"
@@ -29,11 +29,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4_t;
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void_t;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-
-// s_waitcnt with only vmcnt set (bits [3:0] and [15:14])
-#define STEM_WAIT_VMCNT(N) __builtin_amdgcn_s_waitcnt(0x0F70 | ((N) & 15) | (((N) >> 4) << 14))
 
 template <typename T>
 __device__ __forceinline__ f32x4_t product(u32x4_t a, u32x4_t b, f32x4_t c) {
@@ -87,31 +83,54 @@ __device__ __forceinline__ int suffix_len(const PrefixArgs& a, int r) {
 constexpr float kNone = -3e38f;                        // reference of a row that has met no key: below any score, and finite
 constexpr float kSlack = 8.f;                          // how far (in powers of two) scores may pass the reference before it moves
 
-// Rows of a row tile: row m of the KV head is token first + m / G, head m % G of the group.
-template <typename T, int D, int NQ, int WAVES>
-struct RowTile {
+typedef __attribute__((address_space(4))) const int32_t const_i32_t;
+
+// Every wave's reads and writes of LDS are done, and then all waves go on.  (Not __syncthreads, whose fence would wait for the loads
+// that are on their way to registers.)
+#define STEM_LDS_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
+
+// How the waves of a workgroup share its rows and keys: RW groups of 16 NQ rows times KW groups of 32 keys.  With RW = 1 every wave has
+// keys of its own and waits for no other; with RW > 1 the tile of 32 KW keys in LDS is read by RW waves each, and there are two
+// of them in turn, with a barrier per tile.
+template <int NQ_, int RW_, int KW_>
+struct Split {
+    static constexpr int NQ = NQ_, RW = RW_, KW = KW_, kWaves = RW * KW, kRows = 16 * NQ * RW, kKeys = 32 * KW;
+};
+
+template <typename T, int D, typename S>
+struct Part {
+    static constexpr int NQ = S::NQ, RW = S::RW, KW = S::KW, kWaves = S::kWaves;
     static constexpr int kRowBytes = 2 * D;
     static constexpr int kKS = D / 32;                 // 32-wide steps of S^T along d
     static constexpr int kDT = D / 16;                 // 16-column tiles of O^T
-    static constexpr int kHalfBytes = 16 * kRowBytes;  // 16 rows of K or V
-    static constexpr int kStageBytes = 4 * kHalfBytes; // 32 keys of K, then of V
-    static constexpr int kWaveBytes = 2 * kStageBytes;
-    static constexpr int kRows = 16 * NQ;
-    static constexpr int kRequests = kStageBytes / 1024;   // loads of 1 KiB per tile
-    static constexpr int kPerHalf = kHalfBytes / 1024;
+    static constexpr int kTileBytes = S::kKeys * kRowBytes;   // of K, or of V
+    static constexpr int kBuffers = RW > 1 ? 2 : 1;
+    static constexpr int kLdsTiles = kBuffers * 2 * kTileBytes, kLdsJoin = KW > 1 ? KW * S::kRows * D * 4 : 0;
+    static constexpr int kLds = kLdsTiles > kLdsJoin ? kLdsTiles : kLdsJoin;
+    // rows of K and V that a wave fetches of a tile, in pieces of at most 16 (which lie in one page), 1 KiB per load
+    static constexpr int kMyRows = 32 / RW, kPieces = kMyRows > 16 ? 2 : 1, kPieceRows = kMyRows / kPieces;
+    static constexpr int kRowsPerLoad = 1024 / kRowBytes, kLoads = kPieceRows / kRowsPerLoad;
+    static_assert(kLoads >= 1, "a whole load per piece");
 
     u32x4_t q[NQ][kKS];
     f32x4_t o[kDT][NQ];
     float off[NQ], l[NQ];                              // minus the reference, in powers of two; sum of the lane's keys
+    u32x4_t k_in[kPieces][kLoads], v_in[kPieces][kLoads];   // the next tile, on its way
 
     static __device__ __forceinline__ int k_swz(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
     static __device__ __forceinline__ int v_swz(int row) { return D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; }
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    static __device__ __forceinline__ int row_group() { return RW == 1 ? 0 : wave() % RW; }
+    static __device__ __forceinline__ int key_group() { return RW == 1 ? wave() : wave() / RW; }
+    // first row of the tile that this wave fetches
+    static __device__ __forceinline__ int my_row() { return wave() * kMyRows; }
 
+    // Row m of a KV head is token first + m / G, head m % G of the group; m0 is the workgroup's first.
     __device__ __forceinline__ void load_q(const uint16_t* base, int64_t st, int64_t sh, int first, int G, int m0, int m_end) {
         const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            const int m = min(m0 + 16 * n + (lane & 15), m_end - 1), t = m / G;   // rows past the end repeat the last
+            const int m = min(m0 + 16 * (NQ * row_group() + n) + (lane & 15), m_end - 1), t = m / G;   // rows past the end repeat the last
             const uint16_t* row = base + (int64_t)(first + t) * st + (int64_t)(m - t * G) * sh + 8 * (lane >> 4);
 #pragma unroll
             for (int ks = 0; ks < kKS; ++ks) q[n][ks] = *reinterpret_cast<const u32x4_t*>(row + 32 * ks);
@@ -122,30 +141,46 @@ struct RowTile {
         }
     }
 
-    // 16 rows of K or V -> LDS.  The 16-byte chunks of a row are exchanged within it (swz), which spreads the rows that are read together
-    // over the banks; a lane fetches the chunk that belongs at its place.
-    template <bool V>
-    static __device__ __forceinline__ void fetch(const uint16_t* base, int64_t row_stride, int valid, unsigned char* lds) {
+    // Asks for piece x of this wave's rows: `valid` of them are there, at k and v; the others become zeros.
+    __device__ __forceinline__ void fetch(int x, const uint16_t* k, const uint16_t* v, int64_t row_stride, int valid) {
         const int lane = threadIdx.x & 63;
-        constexpr int kChunks = D / 8, kRowsPerLoad = 64 / kChunks;
         const int bytes = valid > 0 ? (int)((valid - 1) * row_stride * 2) + kRowBytes : 0;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, bytes, 0x00020000);
+        const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(k), 0, bytes, 0x00020000);
+        const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(v), 0, bytes, 0x00020000);
+        constexpr int kChunks = D / 8;
 #pragma unroll
-        for (int u = 0; u < kPerHalf; ++u) {
-            const int row = u * kRowsPerLoad + lane / kChunks, c = (lane % kChunks) ^ (V ? v_swz(row) : k_swz(row));
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(lds + u * 1024), 16,
-                                                     (int)(row * row_stride * 2) + c * 16, 0, 0, 0);
+        for (int u = 0; u < kLoads; ++u) {
+            const int at = (int)((u * kRowsPerLoad + lane / kChunks) * row_stride * 2) + (lane % kChunks) * 16;
+            k_in[x][u] = __builtin_amdgcn_raw_buffer_load_b128(rk, at, 0, 0);
+            v_in[x][u] = __builtin_amdgcn_raw_buffer_load_b128(rv, at, 0, 0);
         }
     }
 
-    // One tile of 32 keys that is in LDS.  EDGE: key x of the lane's column counts if x < seen(n) and its half is there.
+    // What has been asked for -> LDS.  The 16-byte chunks of a row are exchanged within it (swz), which spreads the rows that are read
+    // together over the banks.
+    __device__ __forceinline__ void store(unsigned char* lds) {
+        const int lane = threadIdx.x & 63;
+        constexpr int kChunks = D / 8;
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x)
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const int row = my_row() + x * kPieceRows + u * kRowsPerLoad + lane / kChunks, c = lane % kChunks;
+                unsigned char* at = lds + row * kRowBytes;
+                *reinterpret_cast<u32x4_t*>(at + ((c ^ k_swz(row)) << 4)) = k_in[x][u];
+                *reinterpret_cast<u32x4_t*>(at + kTileBytes + ((c ^ v_swz(row)) << 4)) = v_in[x][u];
+            }
+    }
+
+    // This wave's 32 keys of a tile in LDS.  EDGE: key x of query n's column counts if seen(n, x).
     template <bool EDGE, typename Seen>
     __device__ __forceinline__ void tile(const unsigned char* lds, float scale_log2, Seen seen) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4;
+        const unsigned char* mine = lds + key_group() * 32 * kRowBytes;
         f32x4_t s[2][NQ];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            const unsigned char* row = lds + kt * kHalfBytes + c16 * kRowBytes;
+            const unsigned char* row = mine + (16 * kt + c16) * kRowBytes;
 #pragma unroll
             for (int ks = 0; ks < kKS; ++ks) {
                 const u32x4_t k = *reinterpret_cast<const u32x4_t*>(row + (((ks * 4 + grp) ^ k_swz(c16)) << 4));
@@ -191,13 +226,13 @@ struct RowTile {
 #pragma unroll
             for (int x = 0; x < 4; ++x) p[n][x] = pack<T>(f[2 * x], f[2 * x + 1]);
         }
-        const unsigned char* v = lds + 2 * kHalfBytes;
         const int v_row = 4 * grp + (c16 >> 2);
+        const unsigned char* v = mine + kTileBytes + v_row * kRowBytes + (c16 & 1) * 8;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt) {
-            const unsigned char* at = v + v_row * kRowBytes + (((2 * dt + ((c16 >> 1) & 1)) ^ v_swz(v_row)) << 4) + (c16 & 1) * 8;
+            const unsigned char* at = v + (((2 * dt + ((c16 >> 1) & 1)) ^ v_swz(v_row)) << 4);
             const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at);
-            const s16x4_t up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + kHalfBytes));
+            const s16x4_t up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 16 * kRowBytes));
             const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, up);
             const u32x4_t vt = {a.x, a.y, b.x, b.y};
 #pragma unroll
@@ -205,110 +240,113 @@ struct RowTile {
         }
     }
 
+    // Tiles first .. end - 1 of S::kKeys keys, the next one on its way while one is used: ask(t) asks for one, use(t, lds) takes it.
+    template <typename Ask, typename Use>
+    __device__ __forceinline__ void walk(int first, int end, unsigned char* lds, Ask ask, Use use) {
+        if (first >= end) return;
+        ask(first);
+        int buffer = 0;
+        for (int t = first; t < end; ++t) {
+            store(lds + buffer);
+            if (t + 1 < end) ask(t + 1);
+            if constexpr (RW > 1) STEM_LDS_BARRIER();
+            use(t, lds + buffer);
+            if constexpr (RW > 1) buffer ^= 2 * kTileBytes;
+        }
+    }
+
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
     __device__ __forceinline__ void finish(unsigned char* lds, float2* wave_ml, float* part, float2* ml, int m0, int m_end) {
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c16 = lane & 15, grp = lane >> 4;
-        __syncthreads();                               // every wave is done with its tiles
+        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             l[n] += __shfl_xor(l[n], 16);
             l[n] += __shfl_xor(l[n], 32);
-            if (grp == 0) wave_ml[w * kRows + 16 * n + c16] = make_float2(-off[n], l[n]);
         }
-        __syncthreads();
+        if constexpr (KW == 1) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                const int m = m0 + row0 + 16 * n + c16;
+                if (m >= m_end) continue;
+                if (grp == 0) ml[m] = make_float2(-off[n], l[n]);
+#pragma unroll
+                for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(part + (int64_t)m * D + 16 * dt + 4 * grp) = o[dt][n];
+            }
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+            if (grp == 0) wave_ml[kw * S::kRows + row0 + 16 * n + c16] = make_float2(-off[n], l[n]);
+        __syncthreads();                               // every wave is done with its tiles
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            const int row = 16 * n + c16;
+            const int row = row0 + 16 * n + c16;
             float m = wave_ml[row].x;
 #pragma unroll
-            for (int v = 1; v < WAVES; ++v) m = fmaxf(m, wave_ml[v * kRows + row].x);
+            for (int v = 1; v < KW; ++v) m = fmaxf(m, wave_ml[v * S::kRows + row].x);
             const float mine = __builtin_amdgcn_exp2f(-off[n] - m);   // 1 if nothing has been met by any wave
-            if (w == 0 && grp == 0 && m0 + row < m_end) {
+            if (kw == 0 && grp == 0 && m0 + row < m_end) {
                 float sum = 0.f;
 #pragma unroll
-                for (int v = 0; v < WAVES; ++v) {
-                    const float2 x = wave_ml[v * kRows + row];
+                for (int v = 0; v < KW; ++v) {
+                    const float2 x = wave_ml[v * S::kRows + row];
                     sum += x.y * __builtin_amdgcn_exp2f(x.x - m);
                 }
                 ml[m0 + row] = make_float2(m, sum);
             }
-            float* dst = reinterpret_cast<float*>(lds) + (w * kRows + row) * D + 4 * grp;
+            float* dst = reinterpret_cast<float*>(lds) + (kw * S::kRows + row) * D + 4 * grp;
 #pragma unroll
             for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[dt][n] * mine;
         }
         __syncthreads();
-        for (int x = threadIdx.x; x < kRows * D / 4; x += 64 * WAVES) {
-            const int row = x / (D / 4);
-            if (m0 + row >= m_end) break;
+        for (int x = threadIdx.x; x < S::kRows * D / 4; x += 64 * kWaves) {
+            if (m0 + x / (D / 4) >= m_end) break;
             f32x4_t sum = reinterpret_cast<const f32x4_t*>(lds)[x];
 #pragma unroll
-            for (int v = 1; v < WAVES; ++v) sum += reinterpret_cast<const f32x4_t*>(lds)[v * kRows * D / 4 + x];
+            for (int v = 1; v < KW; ++v) sum += reinterpret_cast<const f32x4_t*>(lds)[v * S::kRows * D / 4 + x];
             reinterpret_cast<f32x4_t*>(part)[(int64_t)m0 * (D / 4) + x] = sum;
         }
     }
 };
 
-// Tiles first, first + WAVES, .. before `end` (wave-uniform), one ahead.  fetch(tile, lds) asks for a tile, use(tile, lds) takes it.
-template <int REQUESTS, int STAGE, int WAVES, typename Fetch, typename Use>
-__device__ __forceinline__ void walk_tiles(int first, int end, unsigned char* lds, Fetch fetch, Use use) {
-    if (first >= end) return;
-    fetch(first, lds);
-    int at = 0;
-    for (int t = first; t < end; t += WAVES) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what was read from the other buffer is there
-        if (t + WAVES < end) {
-            fetch(t + WAVES, lds + (at ^ STAGE));
-            STEM_WAIT_VMCNT(REQUESTS);
-        } else {
-            STEM_WAIT_VMCNT(0);
-        }
-        asm volatile("" ::: "memory");
-        use(t, lds + at);
-        at ^= STAGE;
-    }
-}
-
-template <typename T, int D, int NQ, int NS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void prefix_attn_kernel(PrefixArgs a) {
-    constexpr int kMost = NQ > NS ? NQ : NS;
-    __shared__ __align__(1024) unsigned char lds[WAVES * RowTile<T, D, kMost, WAVES>::kWaveBytes];
-    __shared__ float2 wave_ml[WAVES * 16 * kMost];
-    static_assert(sizeof(lds) >= WAVES * 16 * kMost * D * sizeof(float), "the waves' results");
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// SP: how the rows of the prefix are shared, SO: those of a request and its own keys.
+template <typename T, int D, typename SP, typename SO>
+__global__ __launch_bounds__(64 * SP::kWaves) void prefix_attn_kernel(PrefixArgs a) {
+    static_assert(SP::kWaves == SO::kWaves, "one size of workgroup");
+    using PartP = Part<T, D, SP>;
+    using PartO = Part<T, D, SO>;
+    __shared__ __align__(1024) unsigned char lds[PartP::kLds > PartO::kLds ? PartP::kLds : PartO::kLds];
+    __shared__ float2 wave_ml[SP::kRows * SP::KW > SO::kRows * SO::KW ? SP::kRows * SP::KW : SO::kRows * SO::KW];
     const int id = blockIdx.x;
     if (id < a.prefix_groups) {
         // row tiles of the same keys on one XCD (workgroup id modulo 8), one after the other: they share its L2
         const int x = id & 7, y = id >> 3, row_tile = y % a.row_tiles, combo = y / a.row_tiles * 8 + x;
         if (combo >= a.Hkv * a.prefix_splits) return;
-        const int g = combo % a.Hkv, split = combo / a.Hkv;
-        using Tile = RowTile<T, D, NQ, WAVES>;
-        Tile t;
-        const int m0 = row_tile * Tile::kRows;
+        const int g = combo % a.Hkv, split = combo / a.Hkv, m0 = row_tile * SP::kRows;
+        PartP t;
         t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, 0, a.G, m0, a.rows);
         const int key0 = split * a.split_keys, keys = min(a.split_keys, a.prefix_len - key0);
         const uint16_t* k = a.prefix_k + (int64_t)key0 * a.p_st + g * a.p_sh;
         const uint16_t* v = a.prefix_v + (int64_t)key0 * a.p_st + g * a.p_sh;
-        walk_tiles<Tile::kRequests, Tile::kStageBytes, WAVES>(
-            w, (keys + 31) / 32, lds + w * Tile::kWaveBytes,
-            [&](int tile, unsigned char* to) {
+        t.walk(
+            0, (keys + SP::kKeys - 1) / SP::kKeys, lds,
+            [&](int tile) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int key = tile * 32 + 16 * h, valid = min(max(keys - key, 0), 16);
-                    t.template fetch<false>(k + key * a.p_st, a.p_st, valid, to + h * Tile::kHalfBytes);
-                    t.template fetch<true>(v + key * a.p_st, a.p_st, valid, to + (2 + h) * Tile::kHalfBytes);
+                for (int x = 0; x < PartP::kPieces; ++x) {
+                    const int key = tile * SP::kKeys + t.my_row() + x * PartP::kPieceRows;
+                    t.fetch(x, k + key * a.p_st, v + key * a.p_st, a.p_st, min(keys - key, PartP::kPieceRows));
                 }
             },
             [&](int tile, const unsigned char* from) {
-                const int left = keys - tile * 32;
+                const int left = keys - tile * SP::kKeys - t.key_group() * 32;
                 if (left >= 32) t.template tile<false>(from, a.scale_log2, [](int, int) { return true; });
-                else t.template tile<true>(from, a.scale_log2, [&](int, int x) { return x < left; });
+                else if (left > 0) t.template tile<true>(from, a.scale_log2, [&](int, int x) { return x < left; });
             });
         const int64_t place = ((int64_t)split * a.Hkv + g) * a.rows;
         t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
         return;
     }
     // a request's own keys
-    using Tile = RowTile<T, D, NS, WAVES>;
     int at = id - a.prefix_groups;
     const int g = at % a.Hkv;
     at /= a.Hkv;
@@ -317,43 +355,42 @@ __global__ __launch_bounds__(64 * WAVES) void prefix_attn_kernel(PrefixArgs a) {
     const int split = at % a.suffix_splits, r = at / a.suffix_splits;
     int first, n;
     new_tokens(a, r, first, n);
-    const int mine = min(n, a.max_new) * a.G, m0 = row_tile * Tile::kRows;
+    const int mine = min(n, a.max_new) * a.G, m0 = row_tile * SO::kRows;
     if (m0 >= mine) return;
-    const int len = suffix_len(a, r), tiles = (len + 31) / 32;
-    const int each = suffix_split_tiles(tiles, a.suffix_splits, WAVES), tile0 = split * each;
-    if (tile0 >= tiles) return;
-    Tile t;
+    const int len = suffix_len(a, r);
+    const int split_keys = suffix_split_keys(len, a.suffix_splits), key0 = split * split_keys, keys = min(len - key0, split_keys);
+    if (keys <= 0) return;
+    PartO t;
     t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, m0, mine);
     const int lane = threadIdx.x & 63;
-    // keys that the lane's columns see: those up to the token itself
-    int sees[NS];
+    // keys of this part that the lane's columns see: those up to the token itself
+    int sees[SO::NQ];
 #pragma unroll
-    for (int x = 0; x < NS; ++x) sees[x] = len - n + min(m0 + 16 * x + (lane & 15), mine - 1) / a.G + 1;
-    const int least = len - n + m0 / a.G + 1;          // of the tile's rows
-    const int32_t* row = a.table + (int64_t)r * a.table_row;
-    uint32_t there = 0, there_next = 0;                // halves of the tile in use and of the one asked for that are in a page
-    auto fetch = [&](int tile, unsigned char* to) {
-        there = there_next;
-        there_next = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int key = tile * 32 + 16 * h;
-            int valid = min(max(len - key, 0), 16);
-            const int page = valid > 0 ? __builtin_amdgcn_readfirstlane(row[key >> a.page_shift]) : -1;
-            if ((uint32_t)page >= (uint32_t)a.num_pages) valid = 0;
-            if (valid > 0) there_next |= 1u << h;
-            const int64_t at_key = valid > 0 ? (int64_t)page * a.page_st + (int64_t)(key & ((1 << a.page_shift) - 1)) * a.tok_st + g * a.head_st : 0;
-            t.template fetch<false>(a.k_pages + at_key, a.tok_st, valid, to + h * Tile::kHalfBytes);
-            t.template fetch<true>(a.v_pages + at_key, a.tok_st, valid, to + (2 + h) * Tile::kHalfBytes);
-        }
+    for (int x = 0; x < SO::NQ; ++x)
+        sees[x] = len - key0 - n + min(m0 + 16 * (SO::NQ * t.row_group() + x) + (lane & 15), mine - 1) / a.G + 1;
+    const int least = min(len - key0 - n + m0 / a.G + 1, keys);   // of the workgroup's rows
+    const_i32_t* row = (const_i32_t*)(a.table + (int64_t)r * a.table_row);
+    const int mask = (1 << a.page_shift) - 1;
+    auto page_of = [&](int key) {                      // -1: no key of this part, or no page of the cache's
+        const int page = key < keys ? __builtin_amdgcn_readfirstlane(row[(key0 + key) >> a.page_shift]) : -1;
+        return (uint32_t)page < (uint32_t)a.num_pages ? page : -1;
     };
-    walk_tiles<Tile::kRequests, Tile::kStageBytes, WAVES>(
-        tile0 + w, min(tile0 + each, tiles), lds + w * Tile::kWaveBytes, fetch,
+    t.walk(
+        0, (keys + SO::kKeys - 1) / SO::kKeys, lds,
+        [&](int tile) {
+#pragma unroll
+            for (int x = 0; x < PartO::kPieces; ++x) {
+                const int key = tile * SO::kKeys + t.my_row() + x * PartO::kPieceRows, page = page_of(key);
+                const int64_t at_key = page < 0 ? 0 : (int64_t)page * a.page_st + (int64_t)((key0 + key) & mask) * a.tok_st + g * a.head_st;
+                t.fetch(x, a.k_pages + at_key, a.v_pages + at_key, a.tok_st, page < 0 ? 0 : min(keys - key, PartO::kPieceRows));
+            }
+        },
         [&](int tile, const unsigned char* from) {
-            const bool last = tile + WAVES >= min(tile0 + each, tiles);   // then nothing has been asked for behind it
-            const uint32_t have = last ? there_next : there;
-            if (have == 3u && tile * 32 + 32 <= least) t.template tile<false>(from, a.scale_log2, [](int, int) { return true; });
-            else t.template tile<true>(from, a.scale_log2, [&](int nq, int x) { return tile * 32 + x < sees[nq] && (have >> (x >> 4) & 1u); });
+            const int key = tile * SO::kKeys + t.key_group() * 32;
+            const bool lo = page_of(key) >= 0, hi = page_of(key + 16) >= 0;
+            if (lo && hi && key + 32 <= least) t.template tile<false>(from, a.scale_log2, [](int, int) { return true; });
+            else if (lo || hi)
+                t.template tile<true>(from, a.scale_log2, [&](int nq, int x) { return key + x < sees[nq] && (x < 16 ? lo : hi); });
         });
     const int64_t place = ((int64_t)(a.prefix_splits + split) * a.Hkv + g) * a.rows + (int64_t)first * a.G;
     t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
@@ -361,7 +398,7 @@ __global__ __launch_bounds__(64 * WAVES) void prefix_attn_kernel(PrefixArgs a) {
 
 // Joins the parts of a row: D / 4 lanes per row, four values each.
 constexpr int kJoinThreads = 256;
-template <typename T, int D, int WAVES>
+template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
     constexpr int kLanes = D / 4, kRows = kJoinThreads / kLanes;
     const int64_t item = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;   // request, new token, head
@@ -372,11 +409,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
     int first, n;
     new_tokens(a, (int)r, first, n);
     if (i >= n) return;
-    const int tiles = (suffix_len(a, (int)r) + 31) / 32;
+    const int len = suffix_len(a, (int)r);
     int parts = a.prefix_splits;
-    if (tiles > 0) {
-        const int each = suffix_split_tiles(tiles, a.suffix_splits, WAVES);
-        parts += (tiles + each - 1) / each;
+    if (len > 0) {
+        const int each = suffix_split_keys(len, a.suffix_splits);
+        parts += (len + each - 1) / each;
     }
     const int lane = threadIdx.x % kLanes;
     const int64_t step = (int64_t)a.Hkv * a.rows, row = (int64_t)g * a.rows + (int64_t)(first + i) * a.G + (h - g * a.G);
@@ -403,24 +440,29 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
 
 template <typename T, int D>
 static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) {
-    constexpr int WAVES = D == 256 ? 2 : 4;
-    constexpr int kMost = D == 256 ? 2 : 4;
+    constexpr int W = D == 256 ? 4 : 8;                // waves: with head size 256 one per SIMD, which has all registers
+    using Rows16 = Split<1, 1, W>;
+    using Rows32 = Split<1, 2, W / 2>;
+    using Rows64 = Split<2, 2, W / 2>;
+    using Rows128 = Split<2, 4, W / 4>;
     const int64_t own_groups = p.suffix_splits > 0 ? (int64_t)a.requests * a.Hkv * p.suffix_row_tiles * p.suffix_splits : 0;
     const int64_t joins = ((int64_t)a.requests * a.max_new * a.Hq + kJoinThreads / (D / 4) - 1) / (kJoinThreads / (D / 4));
-    if (a.prefix_groups + own_groups > 1 << 23 || joins > 1 << 23) return STEM_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
-    const dim3 grid((unsigned)(a.prefix_groups + own_groups)), block(64 * WAVES);
+    if (a.prefix_groups + own_groups > 1 << 22 || joins > 1 << 23) return STEM_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
+    const dim3 grid((unsigned)(a.prefix_groups + own_groups)), block(64 * W);
     if (grid.x > 0) {
-        const bool short_own = p.suffix_row_tile == 16;
-        if (p.row_tile == 16) hipLaunchKernelGGL((prefix_attn_kernel<T, D, 1, 1, WAVES>), grid, block, 0, stream, a);
-        else if (p.row_tile == 32 && short_own) hipLaunchKernelGGL((prefix_attn_kernel<T, D, 2, 1, WAVES>), grid, block, 0, stream, a);
-        else if (p.row_tile == 32) hipLaunchKernelGGL((prefix_attn_kernel<T, D, 2, 2, WAVES>), grid, block, 0, stream, a);
-        else if constexpr (kMost == 4) {
-            if (short_own) hipLaunchKernelGGL((prefix_attn_kernel<T, D, 4, 1, WAVES>), grid, block, 0, stream, a);
-            else hipLaunchKernelGGL((prefix_attn_kernel<T, D, 4, 4, WAVES>), grid, block, 0, stream, a);
-        }
+#define STEM_PREFIX_LAUNCH(SP, SO) hipLaunchKernelGGL((prefix_attn_kernel<T, D, SP, SO>), grid, block, 0, stream, a)
+        const bool few = p.suffix_row_tile == 16;
+        if (p.row_tile == 16) STEM_PREFIX_LAUNCH(Rows16, Rows16);
+        else if (p.row_tile == 32 && few) STEM_PREFIX_LAUNCH(Rows32, Rows16);
+        else if (p.row_tile == 32) STEM_PREFIX_LAUNCH(Rows32, Rows64);
+        else if (p.row_tile == 64 && few) STEM_PREFIX_LAUNCH(Rows64, Rows16);
+        else if (p.row_tile == 64) STEM_PREFIX_LAUNCH(Rows64, Rows64);
+        else if (few) STEM_PREFIX_LAUNCH(Rows128, Rows16);
+        else STEM_PREFIX_LAUNCH(Rows128, Rows64);
+#undef STEM_PREFIX_LAUNCH
         if (const int st = check_launch()) return st;
     }
-    hipLaunchKernelGGL((join_kernel<T, D, WAVES>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
     return check_launch();
 }
 
