@@ -116,13 +116,22 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     p.row_tiles = (int32_t)((rows + p.row_tile - 1) / p.row_tile);
     p.prefix_splits = p.split_keys = 0;
     if (s.prefix_len > 0 && rows > 0) {
+        // Parts of whole tiles, one to four rounds of workgroups (one runs on a CU at a time): whichever ends first, where a part costs
+        // its tiles and about two more to begin and end.
         const int64_t others = (int64_t)p.row_tiles * s.num_kv_heads;
-        const int64_t wanted = (cus + others - 1) / others;
-        const int64_t tiles = (s.prefix_len + 127) / 128;
-        const int64_t splits = wanted < tiles ? wanted : tiles;
-        const int64_t each = (tiles + splits - 1) / splits;
-        p.split_keys = (int32_t)(each * 128);
-        p.prefix_splits = (int32_t)((tiles + each - 1) / each);
+        const int32_t waves = s.head_dim == 256 ? 4 : 8, row_groups = p.row_tile == 16 ? 1 : p.row_tile == 128 ? 4 : 2;
+        const int64_t tile = 32 * waves / row_groups, tiles = (s.prefix_len + tile - 1) / tile;
+        int64_t best = -1, best_each = 0;
+        for (int rounds = 1; rounds <= 4; ++rounds) {
+            int64_t splits = (int64_t)rounds * cus / others;
+            splits = splits < 1 ? 1 : splits > tiles ? tiles : splits;
+            const int64_t each = (tiles + splits - 1) / splits;
+            splits = (tiles + each - 1) / each;
+            const int64_t cost = (splits * others + cus - 1) / cus * (each + 2);
+            if (best < 0 || cost < best) best = cost, best_each = each;
+        }
+        p.split_keys = (int32_t)(best_each * tile);
+        p.prefix_splits = (int32_t)((tiles + best_each - 1) / best_each);
     }
     const int64_t own_rows = s.max_new * G < rows ? s.max_new * G : rows;
     p.suffix_row_tile = own_rows <= 16 ? 16 : 64;

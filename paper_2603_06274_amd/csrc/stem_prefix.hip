@@ -112,10 +112,11 @@ struct Part {
     static constexpr int kRowsPerLoad = 1024 / kRowBytes, kLoads = kPieceRows / kRowsPerLoad;
     static_assert(kLoads >= 1, "a whole load per piece");
 
+    using Rows = u32x4_t[kPieces][kLoads];             // a wave's rows of K or V, on their way
+
     u32x4_t q[NQ][kKS];
     f32x4_t o[kDT][NQ];
     float off[NQ], l[NQ];                              // minus the reference, in powers of two; sum of the lane's keys
-    u32x4_t k_in[kPieces][kLoads], v_in[kPieces][kLoads];   // the next tile, on its way
 
     static __device__ __forceinline__ int k_swz(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
     static __device__ __forceinline__ int v_swz(int row) { return D == 64 ? ((row >> 1) & 3) << 1 : (row & 7) << 1; }
@@ -141,24 +142,22 @@ struct Part {
         }
     }
 
-    // Asks for piece x of this wave's rows: `valid` of them are there, at k and v; the others become zeros.
-    __device__ __forceinline__ void fetch(int x, const uint16_t* k, const uint16_t* v, int64_t row_stride, int valid) {
+    // Asks for a piece of this wave's rows: `valid` of them are there, from `base` on; the others become zeros.
+    static __device__ __forceinline__ void fetch(u32x4_t (&in)[kLoads], const uint16_t* base, int64_t row_stride, int valid) {
         const int lane = threadIdx.x & 63;
         const int bytes = valid > 0 ? (int)((valid - 1) * row_stride * 2) + kRowBytes : 0;
-        const auto rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(k), 0, bytes, 0x00020000);
-        const auto rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(v), 0, bytes, 0x00020000);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, bytes, 0x00020000);
         constexpr int kChunks = D / 8;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            const int at = (int)((u * kRowsPerLoad + lane / kChunks) * row_stride * 2) + (lane % kChunks) * 16;
-            k_in[x][u] = __builtin_amdgcn_raw_buffer_load_b128(rk, at, 0, 0);
-            v_in[x][u] = __builtin_amdgcn_raw_buffer_load_b128(rv, at, 0, 0);
-        }
+        for (int u = 0; u < kLoads; ++u)
+            in[u] = __builtin_amdgcn_raw_buffer_load_b128(
+                rsrc, (int)((u * kRowsPerLoad + lane / kChunks) * row_stride * 2) + (lane % kChunks) * 16, 0, 0);
     }
 
     // What has been asked for -> LDS.  The 16-byte chunks of a row are exchanged within it (swz), which spreads the rows that are read
     // together over the banks.
-    __device__ __forceinline__ void store(unsigned char* lds) {
+    template <bool V>
+    static __device__ __forceinline__ void store(unsigned char* lds, const Rows& in) {
         const int lane = threadIdx.x & 63;
         constexpr int kChunks = D / 8;
 #pragma unroll
@@ -166,18 +165,14 @@ struct Part {
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
                 const int row = my_row() + x * kPieceRows + u * kRowsPerLoad + lane / kChunks, c = lane % kChunks;
-                unsigned char* at = lds + row * kRowBytes;
-                *reinterpret_cast<u32x4_t*>(at + ((c ^ k_swz(row)) << 4)) = k_in[x][u];
-                *reinterpret_cast<u32x4_t*>(at + kTileBytes + ((c ^ v_swz(row)) << 4)) = v_in[x][u];
+                *reinterpret_cast<u32x4_t*>(lds + row * kRowBytes + ((c ^ (V ? v_swz(row) : k_swz(row))) << 4)) = in[x][u];
             }
     }
 
-    // This wave's 32 keys of a tile in LDS.  EDGE: key x of query n's column counts if seen(n, x).
-    template <bool EDGE, typename Seen>
-    __device__ __forceinline__ void tile(const unsigned char* lds, float scale_log2, Seen seen) {
+    // S^T of this wave's 32 keys of a tile of K in LDS.
+    __device__ __forceinline__ void scores(f32x4_t (&s)[2][NQ], const unsigned char* k_lds) const {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4;
-        const unsigned char* mine = lds + key_group() * 32 * kRowBytes;
-        f32x4_t s[2][NQ];
+        const unsigned char* mine = k_lds + key_group() * 32 * kRowBytes;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             const unsigned char* row = mine + (16 * kt + c16) * kRowBytes;
@@ -189,45 +184,68 @@ struct Part {
                     s[kt][n] = product<T>(k, q[n][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : s[kt][n]);
             }
         }
-        u32x4_t p[NQ];
+    }
+
+    // Scores -> exponents (powers of two over the reference), at most kSlack: where one passes it the reference moves there, and what
+    // has been summed up is scaled.  edge: key x of query n's column counts only if seen(n, x).
+    template <typename Seen>
+    __device__ __forceinline__ void exponents(f32x4_t (&s)[2][NQ], float scale_log2, bool edge, Seen seen) {
+        const int grp = (threadIdx.x & 63) >> 4;
+        if (__builtin_expect(edge, 0)) {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            if constexpr (EDGE) {
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int x = 0; x < 8; ++x)
                     if (!seen(n, (x >> 2) * 16 + 4 * grp + (x & 3))) s[x >> 2][n][x & 3] = -__builtin_huge_valf();
-            }
-            float f[8];
+        }
+        f32x4_t f[2][NQ];
+        bool moves = false;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) f[x] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
-            const float high = max3(max3(f[0], f[1], f[2]), max3(f[3], f[4], f[5]), fmaxf(f[6], f[7]));
-            if (__builtin_expect(__builtin_amdgcn_ballot_w64(high > kSlack) != 0, 0)) {
-                float top = fmaxf(high, __shfl_xor(high, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                if (top > kSlack) {                    // the same in the column's four lanes
+        for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
+            moves |= max3(max3(f[0][n][0], f[0][n][1], f[0][n][2]), max3(f[0][n][3], f[1][n][0], f[1][n][1]),
+                          fmaxf(f[1][n][2], f[1][n][3])) > kSlack;
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(moves) != 0, 0)) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                // the largest of the raw scores: beside the first reference an exponent says nothing
+                float raw = max3(max3(s[0][n][0], s[0][n][1], s[0][n][2]), max3(s[0][n][3], s[1][n][0], s[1][n][1]),
+                                 fmaxf(s[1][n][2], s[1][n][3]));
+                raw = fmaxf(raw, __shfl_xor(raw, 16));
+                raw = fmaxf(raw, __shfl_xor(raw, 32));  // the same in the column's four lanes
+                if (__builtin_fmaf(raw, scale_log2, off[n]) > kSlack) {
                     const float then = off[n];
-                    // the largest of the raw scores: from `high` it would be lost beside the first reference
-                    float raw = max3(max3(s[0][n][0], s[0][n][1], s[0][n][2]), max3(s[0][n][3], s[1][n][0], s[1][n][1]),
-                                     fmaxf(s[1][n][2], s[1][n][3]));
-                    raw = fmaxf(raw, __shfl_xor(raw, 16));
-                    raw = fmaxf(raw, __shfl_xor(raw, 32));
                     off[n] = -raw * scale_log2;
                     const float corr = __builtin_amdgcn_exp2f(off[n] - then);
                     l[n] *= corr;
 #pragma unroll
                     for (int dt = 0; dt < kDT; ++dt) o[dt][n] *= corr;
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) f[x] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
+                    for (int x = 0; x < 8; ++x) f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
                 }
             }
+        }
 #pragma unroll
-            for (int x = 0; x < 8; ++x) f[x] = __builtin_amdgcn_exp2f(f[x]);
-            l[n] += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+        for (int n = 0; n < NQ; ++n) s[0][n] = f[0][n], s[1][n] = f[1][n];
+    }
+
+    // Exponents -> weights, their sums, and o += of this wave's 32 keys of a tile of V in LDS.
+    __device__ __forceinline__ void outputs(const f32x4_t (&f)[2][NQ], const unsigned char* v_lds) {
+        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4;
+        u32x4_t p[NQ];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) p[n][x] = pack<T>(f[2 * x], f[2 * x + 1]);
+        for (int n = 0; n < NQ; ++n) {
+            float w[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) w[x] = __builtin_amdgcn_exp2f(f[x >> 2][n][x & 3]);
+            l[n] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) p[n][x] = pack<T>(w[2 * x], w[2 * x + 1]);
         }
         const int v_row = 4 * grp + (c16 >> 2);
-        const unsigned char* v = mine + kTileBytes + v_row * kRowBytes + (c16 & 1) * 8;
+        const unsigned char* v = v_lds + (key_group() * 32 + v_row) * kRowBytes + (c16 & 1) * 8;
 #pragma unroll
         for (int dt = 0; dt < kDT; ++dt) {
             const unsigned char* at = v + (((2 * dt + ((c16 >> 1) & 1)) ^ v_swz(v_row)) << 4);
@@ -240,19 +258,43 @@ struct Part {
         }
     }
 
-    // Tiles first .. end - 1 of S::kKeys keys, the next one on its way while one is used: ask(t) asks for one, use(t, lds) takes it.
-    template <typename Ask, typename Use>
-    __device__ __forceinline__ void walk(int first, int end, unsigned char* lds, Ask ask, Use use) {
-        if (first >= end) return;
-        ask(first);
-        int buffer = 0;
-        for (int t = first; t < end; ++t) {
-            store(lds + buffer);
-            if (t + 1 < end) ask(t + 1);
+    // All tiles of S::kKeys keys.  ask_k(rows, t) and ask_v ask for a tile (one that does not exist gives zeros); edge(t) says whether
+    // seen(t, n, x) has to be asked for this wave's keys.  While the weights of a tile are formed and used, the scores of the next one
+    // are: its K lies in LDS by then, one more tile of K and the next of V are on their way.
+    template <typename AskK, typename AskV, typename Edge, typename Seen>
+    __device__ __forceinline__ void walk(int tiles, unsigned char* lds, float scale_log2, AskK ask_k, AskV ask_v, Edge edge, Seen seen) {
+        constexpr int kOther = RW > 1 ? kTileBytes : 0;    // from one buffer to the other
+        unsigned char *k_lds = lds, *v_lds = lds + kBuffers * kTileBytes;
+        Rows a, b;
+        ask_k(a, 0);
+        ask_k(b, 1);
+        store<false>(k_lds, a);
+        ask_v(a, 0);
+        if constexpr (RW > 1) STEM_LDS_BARRIER();
+        f32x4_t s[2][NQ];
+        scores(s, k_lds);
+        exponents(s, scale_log2, edge(0), [&](int n, int x) { return seen(0, n, x); });
+        store<false>(k_lds + kOther, b);
+        store<true>(v_lds, a);
+        ask_k(a, 2);
+        ask_v(b, 1);
+        if constexpr (RW > 1) STEM_LDS_BARRIER();
+        int at = 0;                                    // where V of tile t lies, and K of tile t + 2 will
+        for (int t = 0; t + 1 < tiles; ++t) {
+            f32x4_t next[2][NQ];
+            scores(next, k_lds + (at ^ kOther));
+            outputs(s, v_lds + at);
+            exponents(next, scale_log2, edge(t + 1), [&](int n, int x) { return seen(t + 1, n, x); });
+            store<false>(k_lds + at, a);
+            store<true>(v_lds + (at ^ kOther), b);
+            ask_k(a, t + 3);
+            ask_v(b, t + 2);
             if constexpr (RW > 1) STEM_LDS_BARRIER();
-            use(t, lds + buffer);
-            if constexpr (RW > 1) buffer ^= 2 * kTileBytes;
+            at ^= kOther;
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) s[0][n] = next[0][n], s[1][n] = next[1][n];
         }
+        outputs(s, v_lds + at);
     }
 
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
@@ -328,20 +370,18 @@ __global__ __launch_bounds__(64 * SP::kWaves) void prefix_attn_kernel(PrefixArgs
         const int key0 = split * a.split_keys, keys = min(a.split_keys, a.prefix_len - key0);
         const uint16_t* k = a.prefix_k + (int64_t)key0 * a.p_st + g * a.p_sh;
         const uint16_t* v = a.prefix_v + (int64_t)key0 * a.p_st + g * a.p_sh;
-        t.walk(
-            0, (keys + SP::kKeys - 1) / SP::kKeys, lds,
-            [&](int tile) {
+        auto ask = [&](typename PartP::Rows& rows, const uint16_t* base, int tile) {
 #pragma unroll
-                for (int x = 0; x < PartP::kPieces; ++x) {
-                    const int key = tile * SP::kKeys + t.my_row() + x * PartP::kPieceRows;
-                    t.fetch(x, k + key * a.p_st, v + key * a.p_st, a.p_st, min(keys - key, PartP::kPieceRows));
-                }
-            },
-            [&](int tile, const unsigned char* from) {
-                const int left = keys - tile * SP::kKeys - t.key_group() * 32;
-                if (left >= 32) t.template tile<false>(from, a.scale_log2, [](int, int) { return true; });
-                else if (left > 0) t.template tile<true>(from, a.scale_log2, [&](int, int x) { return x < left; });
-            });
+            for (int x = 0; x < PartP::kPieces; ++x) {
+                const int key = tile * SP::kKeys + t.my_row() + x * PartP::kPieceRows;
+                t.fetch(rows[x], base + key * a.p_st, a.p_st, min(keys - key, PartP::kPieceRows));
+            }
+        };
+        const int left = keys - t.key_group() * 32;    // of this wave's keys in tile 0
+        t.walk(
+            (keys + SP::kKeys - 1) / SP::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) { ask(rows, k, tile); },
+            [&](auto& rows, int tile) { ask(rows, v, tile); }, [&](int tile) { return left - tile * SP::kKeys < 32; },
+            [&](int tile, int, int x) { return x < left - tile * SP::kKeys; });
         const int64_t place = ((int64_t)split * a.Hkv + g) * a.rows;
         t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
         return;
@@ -375,58 +415,101 @@ __global__ __launch_bounds__(64 * SP::kWaves) void prefix_attn_kernel(PrefixArgs
         const int page = key < keys ? __builtin_amdgcn_readfirstlane(row[(key0 + key) >> a.page_shift]) : -1;
         return (uint32_t)page < (uint32_t)a.num_pages ? page : -1;
     };
-    t.walk(
-        0, (keys + SO::kKeys - 1) / SO::kKeys, lds,
-        [&](int tile) {
+    auto ask = [&](typename PartO::Rows& rows, const uint16_t* pages, int tile) {
 #pragma unroll
-            for (int x = 0; x < PartO::kPieces; ++x) {
-                const int key = tile * SO::kKeys + t.my_row() + x * PartO::kPieceRows, page = page_of(key);
-                const int64_t at_key = page < 0 ? 0 : (int64_t)page * a.page_st + (int64_t)((key0 + key) & mask) * a.tok_st + g * a.head_st;
-                t.fetch(x, a.k_pages + at_key, a.v_pages + at_key, a.tok_st, page < 0 ? 0 : min(keys - key, PartO::kPieceRows));
-            }
-        },
-        [&](int tile, const unsigned char* from) {
+        for (int x = 0; x < PartO::kPieces; ++x) {
+            const int key = tile * SO::kKeys + t.my_row() + x * PartO::kPieceRows, page = page_of(key);
+            const int64_t at_key = page < 0 ? 0 : (int64_t)page * a.page_st + (int64_t)((key0 + key) & mask) * a.tok_st + g * a.head_st;
+            t.fetch(rows[x], pages + at_key, a.tok_st, page < 0 ? 0 : min(keys - key, PartO::kPieceRows));
+        }
+    };
+    bool lo = false, hi = false;                       // whether the halves of the wave's 32 keys are in a page
+    t.walk(
+        (keys + SO::kKeys - 1) / SO::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) { ask(rows, a.k_pages, tile); },
+        [&](auto& rows, int tile) { ask(rows, a.v_pages, tile); },
+        [&](int tile) {
             const int key = tile * SO::kKeys + t.key_group() * 32;
-            const bool lo = page_of(key) >= 0, hi = page_of(key + 16) >= 0;
-            if (lo && hi && key + 32 <= least) t.template tile<false>(from, a.scale_log2, [](int, int) { return true; });
-            else if (lo || hi)
-                t.template tile<true>(from, a.scale_log2, [&](int nq, int x) { return key + x < sees[nq] && (x < 16 ? lo : hi); });
-        });
+            lo = page_of(key) >= 0, hi = page_of(key + 16) >= 0;
+            return !lo || !hi || key + 32 > least;
+        },
+        [&](int tile, int nq, int x) { return tile * SO::kKeys + t.key_group() * 32 + x < sees[nq] && (x < 16 ? lo : hi); });
     const int64_t place = ((int64_t)(a.prefix_splits + split) * a.Hkv + g) * a.rows + (int64_t)first * a.G;
     t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
 }
 
-// Joins the parts of a row: D / 4 lanes per row, four values each.
+// Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
+// at a time is asked for before any of it is used, as a row waits for memory and does next to nothing else.
 constexpr int kJoinThreads = 256;
-template <typename T, int D>
+template <typename T, int D, int GROUPS>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
-    constexpr int kLanes = D / 4, kRows = kJoinThreads / kLanes;
-    const int64_t item = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;   // request, new token, head
+    constexpr int kLanes = D / 4, kRows = kJoinThreads / (kLanes * GROUPS), kAtOnce = 4;
+    __shared__ f32x4_t group_o[GROUPS > 1 ? kJoinThreads : 1];
+    __shared__ float2 group_ml[GROUPS > 1 ? kRows * GROUPS : 1];
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes % GROUPS, my_row = threadIdx.x / (kLanes * GROUPS);
+    const int64_t item = (int64_t)blockIdx.x * kRows + my_row;   // request, new token, head
     const int per_request = a.max_new * a.Hq;
-    const int64_t r = item / per_request;
-    if (r >= a.requests) return;
-    const int rest = (int)(item - r * per_request), i = rest / a.Hq, h = rest - i * a.Hq, g = h / a.G;
-    int first, n;
-    new_tokens(a, (int)r, first, n);
-    if (i >= n) return;
-    const int len = suffix_len(a, (int)r);
-    int parts = a.prefix_splits;
-    if (len > 0) {
-        const int each = suffix_split_keys(len, a.suffix_splits);
-        parts += (len + each - 1) / each;
+    const int r = (int)(item / per_request), rest = (int)(item - (int64_t)r * per_request), i = rest / a.Hq, h = rest - i * a.Hq, g = h / a.G;
+    int first = 0, n = 0, parts = 0;
+    if (r < a.requests) {
+        new_tokens(a, r, first, n);
+        if (i < n) {
+            const int len = suffix_len(a, r);
+            parts = a.prefix_splits;
+            if (len > 0) {
+                const int each = suffix_split_keys(len, a.suffix_splits);
+                parts += (len + each - 1) / each;
+            }
+        }
     }
-    const int lane = threadIdx.x % kLanes;
     const int64_t step = (int64_t)a.Hkv * a.rows, row = (int64_t)g * a.rows + (int64_t)(first + i) * a.G + (h - g * a.G);
-    float m = kNone;
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, a.part_ml[p * step + row].x);
-    float l = 0.f;
+    float m = kNone, l = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) {
-        const float2 ml = a.part_ml[p * step + row];
-        const float c = __builtin_amdgcn_exp2f(ml.x - m);
-        l += c * ml.y;
-        o += c * reinterpret_cast<const f32x4_t*>(a.part_o + (p * step + row) * D)[lane];
+    for (int p0 = group; p0 < parts; p0 += kAtOnce * GROUPS) {
+        float2 ml[kAtOnce];
+        f32x4_t part[kAtOnce];
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+            const int p = p0 + x * GROUPS;
+            const int64_t at = (p < parts ? p : p0) * step + row;
+            ml[x] = a.part_ml[at];
+            part[x] = reinterpret_cast<const f32x4_t*>(a.part_o + at * D)[lane];
+            if (p >= parts) ml[x] = make_float2(kNone, 0.f);
+        }
+        float top = m;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) top = fmaxf(top, ml[x].x);
+        const float then = __builtin_amdgcn_exp2f(m - top);
+        l *= then;
+        o *= then;
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) {
+            const float c = p0 + x * GROUPS < parts ? __builtin_amdgcn_exp2f(ml[x].x - top) : 0.f;
+            l += c * ml[x].y;
+            if (c != 0.f) o += c * part[x];            // (0 times a part that is not finite is nothing of this row's)
+        }
+        m = top;
     }
+    if constexpr (GROUPS > 1) {
+        group_o[threadIdx.x] = o;
+        if (lane == 0) group_ml[my_row * GROUPS + group] = make_float2(m, l);
+        __syncthreads();
+        if (group > 0) return;
+        float top = m;
+#pragma unroll
+        for (int x = 1; x < GROUPS; ++x) top = fmaxf(top, group_ml[my_row * GROUPS + x].x);
+        const float mine = __builtin_amdgcn_exp2f(m - top);
+        l *= mine;
+        o *= mine;
+#pragma unroll
+        for (int x = 1; x < GROUPS; ++x) {
+            const float2 other = group_ml[my_row * GROUPS + x];
+            const float c = __builtin_amdgcn_exp2f(other.x - top);
+            l += c * other.y;
+            o += c * group_o[threadIdx.x + x * kLanes];
+        }
+        m = top;
+    }
+    if (i >= n) return;                                // (n is 0 behind the last request)
     const bool empty = l == 0.f;
     const float inv = empty ? 0.f : 1.f / l;
     uint2 packed;
@@ -446,7 +529,10 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
     using Rows64 = Split<2, 2, W / 2>;
     using Rows128 = Split<2, 4, W / 4>;
     const int64_t own_groups = p.suffix_splits > 0 ? (int64_t)a.requests * a.Hkv * p.suffix_row_tiles * p.suffix_splits : 0;
-    const int64_t joins = ((int64_t)a.requests * a.max_new * a.Hq + kJoinThreads / (D / 4) - 1) / (kJoinThreads / (D / 4));
+    // several groups of lanes per row where there are parts for them
+    constexpr int kGroups = 4 * kJoinThreads / D;
+    const bool many = p.prefix_splits + p.suffix_splits > 4;
+    const int64_t joined = (int64_t)a.requests * a.max_new * a.Hq, joins = many ? joined : (joined + kGroups - 1) / kGroups;
     if (a.prefix_groups + own_groups > 1 << 22 || joins > 1 << 23) return STEM_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
     const dim3 grid((unsigned)(a.prefix_groups + own_groups)), block(64 * W);
     if (grid.x > 0) {
@@ -462,7 +548,8 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
 #undef STEM_PREFIX_LAUNCH
         if (const int st = check_launch()) return st;
     }
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
+    if (many) hipLaunchKernelGGL((join_kernel<T, D, kGroups>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
+    else hipLaunchKernelGGL((join_kernel<T, D, 1>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
     return check_launch();
 }
 
