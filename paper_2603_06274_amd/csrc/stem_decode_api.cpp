@@ -107,7 +107,7 @@ static int check_prefix(const stem_prefix_shape* s) {
 }
 
 int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
-    const int cus = units();
+    const int cus = units() * (s.head_dim == 256 ? 1 : 2);   // workgroups at a time
     if (cus <= 0) return STEM_ERR_HIP;
     const int64_t G = s.num_q_heads / s.num_kv_heads, rows = s.tokens * G;
     PrefixPlan p;
@@ -119,7 +119,7 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
         // Parts of whole tiles, one to four rounds of workgroups (one runs on a CU at a time): whichever ends first, where a part costs
         // its tiles and about two more to begin and end.
         const int64_t others = (int64_t)p.row_tiles * s.num_kv_heads;
-        const int32_t waves = s.head_dim == 256 ? 4 : 8, row_groups = p.row_tile == 16 ? 1 : p.row_tile == 128 ? 4 : 2;
+        const int32_t waves = 4, row_groups = p.row_tile == 16 ? 1 : p.row_tile == 128 ? 4 : 2;
         const int64_t tile = 32 * waves / row_groups, tiles = (s.prefix_len + tile - 1) / tile;
         int64_t best = -1, best_each = 0;
         for (int rounds = 1; rounds <= 4; ++rounds) {

@@ -279,22 +279,29 @@ struct Part {
         ask_k(a, 2);
         ask_v(b, 1);
         if constexpr (RW > 1) STEM_LDS_BARRIER();
-        int at = 0;                                    // where V of tile t lies, and K of tile t + 2 will
-        for (int t = 0; t + 1 < tiles; ++t) {
-            f32x4_t next[2][NQ];
+        // at: where V of tile t lies, and K of tile t + 2 will
+        auto step = [&](int t, int at, f32x4_t (&f)[2][NQ], f32x4_t (&next)[2][NQ]) __attribute__((always_inline)) {
             scores(next, k_lds + (at ^ kOther));
-            outputs(s, v_lds + at);
+            outputs(f, v_lds + at);
             exponents(next, scale_log2, edge(t + 1), [&](int n, int x) { return seen(t + 1, n, x); });
             store<false>(k_lds + at, a);
             store<true>(v_lds + (at ^ kOther), b);
             ask_k(a, t + 3);
             ask_v(b, t + 2);
             if constexpr (RW > 1) STEM_LDS_BARRIER();
-            at ^= kOther;
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) s[0][n] = next[0][n], s[1][n] = next[1][n];
+        };
+        f32x4_t s2[2][NQ];
+        int t = 0;
+        for (; t + 2 < tiles; t += 2) {
+            step(t, 0, s, s2);
+            step(t + 1, kOther, s2, s);
         }
-        outputs(s, v_lds + at);
+        if (t + 1 < tiles) {
+            step(t, 0, s, s2);
+            outputs(s2, v_lds + kOther);
+        } else {
+            outputs(s, v_lds);
+        }
     }
 
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
@@ -353,7 +360,7 @@ struct Part {
 
 // SP: how the rows of the prefix are shared, SO: those of a request and its own keys.
 template <typename T, int D, typename SP, typename SO>
-__global__ __launch_bounds__(64 * SP::kWaves) void prefix_attn_kernel(PrefixArgs a) {
+__global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn_kernel(PrefixArgs a) {
     static_assert(SP::kWaves == SO::kWaves, "one size of workgroup");
     using PartP = Part<T, D, SP>;
     using PartO = Part<T, D, SO>;
@@ -523,7 +530,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
 
 template <typename T, int D>
 static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) {
-    constexpr int W = D == 256 ? 4 : 8;                // waves: with head size 256 one per SIMD, which has all registers
+    constexpr int W = 4;
     using Rows16 = Split<1, 1, W>;
     using Rows32 = Split<1, 2, W / 2>;
     using Rows64 = Split<2, 2, W / 2>;
