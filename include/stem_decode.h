@@ -185,7 +185,7 @@ int stem_prefix_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* hos
  *   - The same inputs give the same bits; what the rest of the batch holds has no influence on a row beyond rounding.
  * workspace: 16-byte aligned, of stem_prefix_attn_workspace_bytes (which depends on the current device), this call's alone until its work has
  * finished.  prefix_k and prefix_v may be NULL if prefix_len is 0; k_pages, v_pages, table and lens if max_suffix is 0.
- * STEM_ERR_UNSUPPORTED if 16 rows span 2 GiB or more.
+ * STEM_ERR_UNSUPPORTED if 16 rows of a page or 128 of the prefix span 2 GiB or more.
  */
 int stem_prefix_attn(const stem_prefix_shape* shape, const void* q, const void* prefix_k, const void* prefix_v,
                      const void* k_pages, const void* v_pages, const int32_t* table, const int32_t* lens,

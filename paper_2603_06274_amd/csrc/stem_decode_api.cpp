@@ -90,11 +90,11 @@ static int check_prefix(const stem_prefix_shape* s) {
     if ((int64_t)s->tokens * s->num_q_heads > kInt32Max || (int64_t)s->max_new * s->num_q_heads > kInt32Max)
         return STEM_ERR_UNSUPPORTED;
     if (!good_strides(s->q_stride_token, s->q_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
-    // the kernel addresses 16 rows through a 32-bit byte offset
-    const int64_t most = (kInt32Max - 2 * s->head_dim) / (2 * 15);
+    // the kernel addresses a tile of the prefix (128 rows at most), and 16 rows of a page, through a 32-bit byte offset
+    const int64_t most = (kInt32Max - 2 * s->head_dim) / (2 * 15), most_prefix = kInt32Max / (2 * 128);
     if (s->prefix_len > 0) {
         if (!good_strides(s->prefix_stride_token, s->prefix_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
-        if (s->prefix_stride_token > most) return STEM_ERR_UNSUPPORTED;
+        if (s->prefix_stride_token > most_prefix) return STEM_ERR_UNSUPPORTED;
     }
     if (s->max_suffix > 0) {
         if (const int st = check_pages(s->pages, s->head_dim)) return st;
@@ -121,11 +121,13 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
         const int64_t others = (int64_t)p.row_tiles * s.num_kv_heads;
         const int32_t waves = 4, row_groups = p.row_tile == 16 ? 1 : p.row_tile == 128 ? 4 : 2;
         const int64_t tile = 32 * waves / row_groups, tiles = (s.prefix_len + tile - 1) / tile;
+        const int64_t most_each = kInt32Max / (2 * s.prefix_stride_token * tile);   // a part's rows: 32-bit byte offsets
         int64_t best = -1, best_each = 0;
         for (int rounds = 1; rounds <= 4; ++rounds) {
             int64_t splits = (int64_t)rounds * cus / others;
             splits = splits < 1 ? 1 : splits > tiles ? tiles : splits;
-            const int64_t each = (tiles + splits - 1) / splits;
+            int64_t each = (tiles + splits - 1) / splits;
+            each = each < most_each ? each : most_each;
             splits = (tiles + each - 1) / each;
             const int64_t cost = (splits * others + cus - 1) / cus * (each + 2);
             if (best < 0 || cost < best) best = cost, best_each = each;

@@ -16,10 +16,24 @@
 // buffer resource whose size ends with the last valid one: rows behind it, and all of a page that is none, arrive as zeros and
 // are masked.  A tile begins at a multiple of 16 keys, so 16 rows lie in one page.
 #include <type_traits>
+#include <utility>
 
 #include "stem_decode_common.h"
 
 namespace stem {
+
+// f(0), f(1), .. f(N - 1) with compile-time arguments
+#define STEM_INLINE __attribute__((always_inline))
+template <typename F, int... I>
+__device__ __forceinline__ void for_each_constant(std::integer_sequence<int, I...>, F&& f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F&& f) {
+    for_each_constant(std::make_integer_sequence<int, N>{}, f);
+}
+// Nothing is scheduled across this point.
+#define STEM_SCHED_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
 typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8_t;
@@ -142,16 +156,18 @@ struct Part {
         }
     }
 
-    // Asks for a piece of this wave's rows: `valid` of them are there, from `base` on; the others become zeros.
-    static __device__ __forceinline__ void fetch(u32x4_t (&in)[kLoads], const uint16_t* base, int64_t row_stride, int valid) {
+    // Asks for a piece of this wave's rows, from `first` bytes behind the resource's begin on; what lies behind its end becomes zeros.
+    static __device__ __forceinline__ void fetch(u32x4_t (&in)[kLoads], __amdgpu_buffer_rsrc_t rsrc, uint32_t row_bytes, uint32_t first) {
         const int lane = threadIdx.x & 63;
-        const int bytes = valid > 0 ? (int)((valid - 1) * row_stride * 2) + kRowBytes : 0;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, bytes, 0x00020000);
         constexpr int kChunks = D / 8;
+        const uint32_t at = lane / kChunks * row_bytes + lane % kChunks * 16;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            in[u] = __builtin_amdgcn_raw_buffer_load_b128(
-                rsrc, (int)((u * kRowsPerLoad + lane / kChunks) * row_stride * 2) + (lane % kChunks) * 16, 0, 0);
+            in[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, first + u * kRowsPerLoad * row_bytes, 0);
+    }
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_resource(const uint16_t* base, uint32_t row_bytes, int rows) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, rows > 0 ? (int)((rows - 1) * row_bytes) + kRowBytes : 0,
+                                                 0x00020000);
     }
 
     // What has been asked for -> LDS.  The 16-byte chunks of a row are exchanged within it (swz), which spreads the rows that are read
@@ -169,92 +185,73 @@ struct Part {
             }
     }
 
-    // S^T of this wave's 32 keys of a tile of K in LDS.
-    __device__ __forceinline__ void scores(f32x4_t (&s)[2][NQ], const unsigned char* k_lds) const {
+    // Operand m of S^T of this wave's 32 keys: 16 keys m / kKS of them, 32-wide step m % kKS along d.
+    static __device__ __forceinline__ u32x4_t load_k(const unsigned char* k_lds, int m) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4;
-        const unsigned char* mine = k_lds + key_group() * 32 * kRowBytes;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            const unsigned char* row = mine + (16 * kt + c16) * kRowBytes;
-#pragma unroll
-            for (int ks = 0; ks < kKS; ++ks) {
-                const u32x4_t k = *reinterpret_cast<const u32x4_t*>(row + (((ks * 4 + grp) ^ k_swz(c16)) << 4));
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-                    s[kt][n] = product<T>(k, q[n][ks], ks == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : s[kt][n]);
-            }
-        }
+        const int at = (key_group() * 32 + c16) * kRowBytes + ((grp ^ k_swz(c16)) << 4);
+        return *reinterpret_cast<const u32x4_t*>(k_lds + (at ^ (m % kKS << 6)) + m / kKS * 16 * kRowBytes);
+    }
+    // Operand dt of O^T: 16 columns of the wave's 32 rows of V, in two transposing reads.
+    static __device__ __forceinline__ u32x4_t load_v(const unsigned char* v_lds, int dt) {
+        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, row = 4 * grp + (c16 >> 2);
+        const int at = (key_group() * 32 + row) * kRowBytes + ((((c16 >> 1) & 1) ^ v_swz(row)) << 4) + (c16 & 1) * 8;
+        const unsigned char* p = v_lds + (at ^ (dt << 5));
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)p);
+        const s16x4_t up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p + 16 * kRowBytes));
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, up);
+        return u32x4_t{a.x, a.y, b.x, b.y};
     }
 
-    // Scores -> exponents (powers of two over the reference), at most kSlack: where one passes it the reference moves there, and what
-    // has been summed up is scaled.  edge: key x of query n's column counts only if seen(n, x).
-    template <typename Seen>
-    __device__ __forceinline__ void exponents(f32x4_t (&s)[2][NQ], float scale_log2, bool edge, Seen seen) {
-        const int grp = (threadIdx.x & 63) >> 4;
-        if (__builtin_expect(edge, 0)) {
+    using Scores = f32x4_t[2][NQ];                     // [16 keys][query tile], or exponents
+
+    __device__ __forceinline__ void exponents_of(Scores& f, const Scores& s, int n, float scale_log2) const {
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
+        for (int x = 0; x < 8; ++x) f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
+    }
+    static __device__ __forceinline__ float largest(const Scores& s, int n) {
+        return max3(max3(s[0][n][0], s[0][n][1], s[0][n][2]), max3(s[0][n][3], s[1][n][0], s[1][n][1]), fmaxf(s[1][n][2], s[1][n][3]));
+    }
+
+    // The exponents f of scores s (powers of two over the reference) are to be at most kSlack: where one passes it the reference moves
+    // there, and what has been summed up is scaled.  edge: key x of query n's column counts only if seen(n, x).
+    template <typename Seen>
+    __device__ __forceinline__ void keep_in_range(Scores& f, Scores& s, float scale_log2, bool edge, Seen seen) {
+        bool moves = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) moves |= largest(f, n) > kSlack;
+        if (__builtin_expect(!edge & (__builtin_amdgcn_ballot_w64(moves) == 0), 1)) return;
+        const int grp = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            if (edge) {
 #pragma unroll
                 for (int x = 0; x < 8; ++x)
                     if (!seen(n, (x >> 2) * 16 + 4 * grp + (x & 3))) s[x >> 2][n][x & 3] = -__builtin_huge_valf();
-        }
-        f32x4_t f[2][NQ];
-        bool moves = false;
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-            for (int x = 0; x < 8; ++x) f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
-            moves |= max3(max3(f[0][n][0], f[0][n][1], f[0][n][2]), max3(f[0][n][3], f[1][n][0], f[1][n][1]),
-                          fmaxf(f[1][n][2], f[1][n][3])) > kSlack;
-        }
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(moves) != 0, 0)) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                // the largest of the raw scores: beside the first reference an exponent says nothing
-                float raw = max3(max3(s[0][n][0], s[0][n][1], s[0][n][2]), max3(s[0][n][3], s[1][n][0], s[1][n][1]),
-                                 fmaxf(s[1][n][2], s[1][n][3]));
-                raw = fmaxf(raw, __shfl_xor(raw, 16));
-                raw = fmaxf(raw, __shfl_xor(raw, 32));  // the same in the column's four lanes
-                if (__builtin_fmaf(raw, scale_log2, off[n]) > kSlack) {
-                    const float then = off[n];
-                    off[n] = -raw * scale_log2;
-                    const float corr = __builtin_amdgcn_exp2f(off[n] - then);
-                    l[n] *= corr;
-#pragma unroll
-                    for (int dt = 0; dt < kDT; ++dt) o[dt][n] *= corr;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
-                }
             }
-        }
+            // the largest of the raw scores: beside the first reference an exponent says nothing
+            float raw = largest(s, n);
+            raw = fmaxf(raw, __shfl_xor(raw, 16));
+            raw = fmaxf(raw, __shfl_xor(raw, 32));      // the same in the column's four lanes
+            if (__builtin_fmaf(raw, scale_log2, off[n]) > kSlack) {
+                const float then = off[n];
+                off[n] = -raw * scale_log2;
+                const float corr = __builtin_amdgcn_exp2f(off[n] - then);
+                l[n] *= corr;
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) s[0][n] = f[0][n], s[1][n] = f[1][n];
+                for (int dt = 0; dt < kDT; ++dt) o[dt][n] *= corr;
+            }
+            exponents_of(f, s, n, scale_log2);
+        }
     }
 
-    // Exponents -> weights, their sums, and o += of this wave's 32 keys of a tile of V in LDS.
-    __device__ __forceinline__ void outputs(const f32x4_t (&f)[2][NQ], const unsigned char* v_lds) {
-        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4;
-        u32x4_t p[NQ];
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            float w[8];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) w[x] = __builtin_amdgcn_exp2f(f[x >> 2][n][x & 3]);
-            l[n] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-#pragma unroll
-            for (int x = 0; x < 4; ++x) p[n][x] = pack<T>(w[2 * x], w[2 * x + 1]);
-        }
-        const int v_row = 4 * grp + (c16 >> 2);
-        const unsigned char* v = v_lds + (key_group() * 32 + v_row) * kRowBytes + (c16 & 1) * 8;
-#pragma unroll
-        for (int dt = 0; dt < kDT; ++dt) {
-            const unsigned char* at = v + (((2 * dt + ((c16 >> 1) & 1)) ^ v_swz(v_row)) << 4);
-            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)at);
-            const s16x4_t up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(at + 16 * kRowBytes));
-            const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, up);
-            const u32x4_t vt = {a.x, a.y, b.x, b.y};
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(vt, p[n], o[dt][n]);
+    // Weight x of a lane's 8 NQ (key x % 8 of query tile x / 8): 2^exponent, into its sum and its place in P^T.
+    __device__ __forceinline__ void weight(Scores& f, u32x4_t (&p)[NQ], int x) {
+        const int n = x >> 3, y = x & 7;
+        f[y >> 2][n][y & 3] = __builtin_amdgcn_exp2f(f[y >> 2][n][y & 3]);
+        if (y & 1) {
+            const float a = f[y >> 2][n][(y & 3) - 1], b = f[y >> 2][n][y & 3];
+            l[n] += a + b;
+            p[n][y >> 1] = pack<T>(a, b);
         }
     }
 
@@ -264,6 +261,8 @@ struct Part {
     template <typename AskK, typename AskV, typename Edge, typename Seen>
     __device__ __forceinline__ void walk(int tiles, unsigned char* lds, float scale_log2, AskK ask_k, AskV ask_v, Edge edge, Seen seen) {
         constexpr int kOther = RW > 1 ? kTileBytes : 0;    // from one buffer to the other
+        constexpr int kS = 2 * kKS;                        // operands of S^T; those of O^T are kDT, as many
+        const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
         unsigned char *k_lds = lds, *v_lds = lds + kBuffers * kTileBytes;
         Rows a, b;
         ask_k(a, 0);
@@ -271,37 +270,65 @@ struct Part {
         store<false>(k_lds, a);
         ask_v(a, 0);
         if constexpr (RW > 1) STEM_LDS_BARRIER();
-        f32x4_t s[2][NQ];
-        scores(s, k_lds);
-        exponents(s, scale_log2, edge(0), [&](int n, int x) { return seen(0, n, x); });
+        Scores f, s;
+#pragma unroll
+        for (int m = 0; m < kS; ++m) {
+            const u32x4_t k = load_k(k_lds, m);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(k, q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) exponents_of(f, s, n, scale_log2);
+        keep_in_range(f, s, scale_log2, edge(0), [&](int n, int x) { return seen(0, n, x); });
         store<false>(k_lds + kOther, b);
         store<true>(v_lds, a);
         ask_k(a, 2);
         ask_v(b, 1);
         if constexpr (RW > 1) STEM_LDS_BARRIER();
-        // at: where V of tile t lies, and K of tile t + 2 will
-        auto step = [&](int t, int at, f32x4_t (&f)[2][NQ], f32x4_t (&next)[2][NQ]) __attribute__((always_inline)) {
-            scores(next, k_lds + (at ^ kOther));
-            outputs(f, v_lds + at);
-            exponents(next, scale_log2, edge(t + 1), [&](int n, int x) { return seen(t + 1, n, x); });
+        // at: where V of tile t lies, and K of tile t + 2 will.  All operands of S^T are read first, then under each of its products
+        // an operand of O^T and a share of the weights; the next exponents under the products of O^T.
+        auto step = [&](int t, int at) STEM_INLINE {
+            u32x4_t k[kS], v[kDT], p[NQ];
+            unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_lds + (at ^ kOther), m); });
+            STEM_SCHED_FENCE();
+            unrolled<kS>([&](auto m_tag) STEM_INLINE {
+                constexpr int m = decltype(m_tag)::value, kPer = 8 * NQ / kS > 0 ? 8 * NQ / kS : 1;
+                v[m] = load_v(v_lds + at, m);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(k[m], q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
+#pragma unroll
+                for (int x = m * kPer; x < (m + 1) * kPer && x < 8 * NQ; ++x) weight(f, p, x);
+                STEM_SCHED_FENCE();
+            });
+            unrolled<kDT>([&](auto dt) STEM_INLINE {
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(v[dt], p[n], o[dt][n]);
+            });
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) exponents_of(f, s, n, scale_log2);
+            keep_in_range(f, s, scale_log2, edge(t + 1), [&](int n, int x) { return seen(t + 1, n, x); });
             store<false>(k_lds + at, a);
             store<true>(v_lds + (at ^ kOther), b);
             ask_k(a, t + 3);
             ask_v(b, t + 2);
             if constexpr (RW > 1) STEM_LDS_BARRIER();
         };
-        f32x4_t s2[2][NQ];
         int t = 0;
         for (; t + 2 < tiles; t += 2) {
-            step(t, 0, s, s2);
-            step(t + 1, kOther, s2, s);
+            step(t, 0);
+            step(t + 1, kOther);
         }
         if (t + 1 < tiles) {
-            step(t, 0, s, s2);
-            outputs(s2, v_lds + kOther);
-        } else {
-            outputs(s, v_lds);
+            step(t, 0);
+            ++t;
         }
+        u32x4_t p[NQ];
+        unrolled<8 * NQ>([&](auto x) STEM_INLINE { weight(f, p, x); });
+        unrolled<kDT>([&](auto dt) STEM_INLINE {
+            const u32x4_t v = load_v(v_lds + (t & 1 ? kOther : 0), dt);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(v, p[n], o[dt][n]);
+        });
     }
 
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
@@ -377,17 +404,19 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
         const int key0 = split * a.split_keys, keys = min(a.split_keys, a.prefix_len - key0);
         const uint16_t* k = a.prefix_k + (int64_t)key0 * a.p_st + g * a.p_sh;
         const uint16_t* v = a.prefix_v + (int64_t)key0 * a.p_st + g * a.p_sh;
-        auto ask = [&](typename PartP::Rows& rows, const uint16_t* base, int tile) {
+        const uint32_t row_bytes = (uint32_t)a.p_st * 2;
+        const auto rk = PartP::rows_resource(k, row_bytes, keys), rv = PartP::rows_resource(v, row_bytes, keys);
+        const int tiles = (keys + SP::kKeys - 1) / SP::kKeys;
+        auto ask = [&](typename PartP::Rows& rows, __amdgpu_buffer_rsrc_t rsrc, int tile) STEM_INLINE {
+            // behind the last tile there is nothing (and its offset is within 32 bits, which those further on need not be)
+            const uint32_t first = (uint32_t)(min(tile, tiles) * SP::kKeys + t.my_row()) * row_bytes;
 #pragma unroll
-            for (int x = 0; x < PartP::kPieces; ++x) {
-                const int key = tile * SP::kKeys + t.my_row() + x * PartP::kPieceRows;
-                t.fetch(rows[x], base + key * a.p_st, a.p_st, min(keys - key, PartP::kPieceRows));
-            }
+            for (int x = 0; x < PartP::kPieces; ++x) t.fetch(rows[x], rsrc, row_bytes, first + x * PartP::kPieceRows * row_bytes);
         };
         const int left = keys - t.key_group() * 32;    // of this wave's keys in tile 0
         t.walk(
-            (keys + SP::kKeys - 1) / SP::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) { ask(rows, k, tile); },
-            [&](auto& rows, int tile) { ask(rows, v, tile); }, [&](int tile) { return left - tile * SP::kKeys < 32; },
+            tiles, lds, a.scale_log2, [&](auto& rows, int tile) STEM_INLINE { ask(rows, rk, tile); },
+            [&](auto& rows, int tile) STEM_INLINE { ask(rows, rv, tile); }, [&](int tile) { return left - tile * SP::kKeys < 32; },
             [&](int tile, int, int x) { return x < left - tile * SP::kKeys; });
         const int64_t place = ((int64_t)split * a.Hkv + g) * a.rows;
         t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
@@ -422,18 +451,19 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
         const int page = key < keys ? __builtin_amdgcn_readfirstlane(row[(key0 + key) >> a.page_shift]) : -1;
         return (uint32_t)page < (uint32_t)a.num_pages ? page : -1;
     };
-    auto ask = [&](typename PartO::Rows& rows, const uint16_t* pages, int tile) {
+    const uint32_t row_bytes = (uint32_t)a.tok_st * 2;
+    auto ask = [&](typename PartO::Rows& rows, const uint16_t* pages, int tile) STEM_INLINE {
 #pragma unroll
         for (int x = 0; x < PartO::kPieces; ++x) {
             const int key = tile * SO::kKeys + t.my_row() + x * PartO::kPieceRows, page = page_of(key);
             const int64_t at_key = page < 0 ? 0 : (int64_t)page * a.page_st + (int64_t)((key0 + key) & mask) * a.tok_st + g * a.head_st;
-            t.fetch(rows[x], pages + at_key, a.tok_st, page < 0 ? 0 : min(keys - key, PartO::kPieceRows));
+            t.fetch(rows[x], PartO::rows_resource(pages + at_key, row_bytes, page < 0 ? 0 : min(keys - key, PartO::kPieceRows)), row_bytes, 0);
         }
     };
     bool lo = false, hi = false;                       // whether the halves of the wave's 32 keys are in a page
     t.walk(
-        (keys + SO::kKeys - 1) / SO::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) { ask(rows, a.k_pages, tile); },
-        [&](auto& rows, int tile) { ask(rows, a.v_pages, tile); },
+        (keys + SO::kKeys - 1) / SO::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) STEM_INLINE { ask(rows, a.k_pages, tile); },
+        [&](auto& rows, int tile) STEM_INLINE { ask(rows, a.v_pages, tile); },
         [&](int tile) {
             const int key = tile * SO::kKeys + t.key_group() * 32;
             lo = page_of(key) >= 0, hi = page_of(key + 16) >= 0;
