@@ -118,8 +118,11 @@ struct Part {
     static constexpr int kKS = D / 32;                 // 32-wide steps of S^T along d
     static constexpr int kDT = D / 16;                 // 16-column tiles of O^T
     static constexpr int kTileBytes = S::kKeys * kRowBytes;   // of K, or of V
-    static constexpr int kBuffers = RW > 1 ? 2 : 1;
-    static constexpr int kLdsTiles = kBuffers * 2 * kTileBytes, kLdsJoin = KW > 1 ? KW * S::kRows * D * 4 : 0;
+    // tiles of K and of V in LDS.  kAhead: the operands of the next S^T are read a step ahead, under the products of O^T, so that
+    // a step has them when it begins; four tiles of K then.
+    static constexpr bool kAhead = RW == 4;
+    static constexpr int kBuffersV = RW > 1 ? 2 : 1, kBuffersK = kAhead ? 4 : kBuffersV;
+    static constexpr int kLdsTiles = (kBuffersK + kBuffersV) * kTileBytes, kLdsJoin = KW > 1 ? KW * S::kRows * D * 4 : 0;
     static constexpr int kLds = kLdsTiles > kLdsJoin ? kLdsTiles : kLdsJoin;
     // rows of K and V that a wave fetches of a tile, in pieces of at most 16 (which lie in one page), 1 KiB per load
     static constexpr int kMyRows = 32 / RW, kPieces = kMyRows > 16 ? 2 : 1, kPieceRows = kMyRows / kPieces;
@@ -260,40 +263,47 @@ struct Part {
     // are: its K lies in LDS by then, one more tile of K and the next of V are on their way.
     template <typename AskK, typename AskV, typename Edge, typename Seen>
     __device__ __forceinline__ void walk(int tiles, unsigned char* lds, float scale_log2, AskK ask_k, AskV ask_v, Edge edge, Seen seen) {
-        constexpr int kOther = RW > 1 ? kTileBytes : 0;    // from one buffer to the other
         constexpr int kS = 2 * kKS;                        // operands of S^T; those of O^T are kDT, as many
         const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
-        unsigned char *k_lds = lds, *v_lds = lds + kBuffers * kTileBytes;
+        auto k_at = [&](int t) STEM_INLINE { return lds + t % kBuffersK * kTileBytes; };
+        auto v_at = [&](int t) STEM_INLINE { return lds + (kBuffersK + t % kBuffersV) * kTileBytes; };
+        auto barrier = []() STEM_INLINE {
+            if constexpr (RW > 1) STEM_LDS_BARRIER();
+        };
         Rows a, b;
+        Scores f, s;
+        u32x4_t k[kS];
         ask_k(a, 0);
         ask_k(b, 1);
-        store<false>(k_lds, a);
+        store<false>(k_at(0), a);
+        if constexpr (kAhead) store<false>(k_at(1), b);
         ask_v(a, 0);
-        if constexpr (RW > 1) STEM_LDS_BARRIER();
-        Scores f, s;
+        if constexpr (kAhead) ask_k(b, 2);
+        barrier();
 #pragma unroll
         for (int m = 0; m < kS; ++m) {
-            const u32x4_t k = load_k(k_lds, m);
+            const u32x4_t first = load_k(k_at(0), m);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(k, q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
+            for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(first, q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
         }
 #pragma unroll
         for (int n = 0; n < NQ; ++n) exponents_of(f, s, n, scale_log2);
         keep_in_range(f, s, scale_log2, edge(0), [&](int n, int x) { return seen(0, n, x); });
-        store<false>(k_lds + kOther, b);
-        store<true>(v_lds, a);
-        ask_k(a, 2);
+        if constexpr (kAhead) unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(1), m); });
+        store<false>(k_at(kAhead ? 2 : 1), b);
+        store<true>(v_at(0), a);
+        ask_k(a, kAhead ? 3 : 2);
         ask_v(b, 1);
-        if constexpr (RW > 1) STEM_LDS_BARRIER();
-        // at: where V of tile t lies, and K of tile t + 2 will.  All operands of S^T are read first, then under each of its products
-        // an operand of O^T and a share of the weights; the next exponents under the products of O^T.
-        auto step = [&](int t, int at) STEM_INLINE {
-            u32x4_t k[kS], v[kDT], p[NQ];
-            unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_lds + (at ^ kOther), m); });
+        barrier();
+        // All operands of S^T are read first, then under each of its products an operand of O^T and a share of the weights; the next
+        // exponents under the products of O^T.  j: t modulo 4.
+        auto step = [&](int t, auto j) STEM_INLINE {
+            u32x4_t v[kDT], p[NQ];
+            if constexpr (!kAhead) unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(j + 1), m); });
             STEM_SCHED_FENCE();
             unrolled<kS>([&](auto m_tag) STEM_INLINE {
                 constexpr int m = decltype(m_tag)::value, kPer = 8 * NQ / kS > 0 ? 8 * NQ / kS : 1;
-                v[m] = load_v(v_lds + at, m);
+                v[m] = load_v(v_at(j), m);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(k[m], q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
 #pragma unroll
@@ -303,29 +313,35 @@ struct Part {
             unrolled<kDT>([&](auto dt) STEM_INLINE {
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(v[dt], p[n], o[dt][n]);
-            });
+                if constexpr (kAhead) k[dt] = load_k(k_at(j + 2), dt);
+                constexpr int kPer = 8 * NQ / kDT > 0 ? 8 * NQ / kDT : 1;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) exponents_of(f, s, n, scale_log2);
+                for (int x = dt * kPer; x < (dt + 1) * kPer && x < 8 * NQ; ++x)
+                    f[x >> 2 & 1][x >> 3][x & 3] = __builtin_fmaf(s[x >> 2 & 1][x >> 3][x & 3], scale_log2, off[x >> 3]);
+                STEM_SCHED_FENCE();
+            });
             keep_in_range(f, s, scale_log2, edge(t + 1), [&](int n, int x) { return seen(t + 1, n, x); });
-            store<false>(k_lds + at, a);
-            store<true>(v_lds + (at ^ kOther), b);
-            ask_k(a, t + 3);
+            store<false>(k_at(kAhead ? j + 3 : j + 2), a);
+            store<true>(v_at(j + 1), b);
+            ask_k(a, kAhead ? t + 4 : t + 3);
             ask_v(b, t + 2);
-            if constexpr (RW > 1) STEM_LDS_BARRIER();
+            barrier();
         };
+        constexpr int kUnroll = kAhead ? 4 : RW > 1 ? 2 : 1;
         int t = 0;
-        for (; t + 2 < tiles; t += 2) {
-            step(t, 0);
-            step(t + 1, kOther);
-        }
-        if (t + 1 < tiles) {
-            step(t, 0);
-            ++t;
-        }
+        for (; t + kUnroll < tiles; t += kUnroll) unrolled<kUnroll>([&](auto j) STEM_INLINE { step(t + j, j); });
+        int last = 0;                                      // t modulo kBuffersV
+        unrolled<kUnroll - 1>([&](auto j) STEM_INLINE {
+            if (t + 1 < tiles) {
+                step(t, j);
+                ++t;
+                last ^= kBuffersV - 1;
+            }
+        });
         u32x4_t p[NQ];
         unrolled<8 * NQ>([&](auto x) STEM_INLINE { weight(f, p, x); });
         unrolled<kDT>([&](auto dt) STEM_INLINE {
-            const u32x4_t v = load_v(v_lds + (t & 1 ? kOther : 0), dt);
+            const u32x4_t v = load_v(v_at(last), dt);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(v, p[n], o[dt][n]);
         });
