@@ -99,6 +99,10 @@ constexpr float kSlack = 8.f;                          // how far (in powers of 
 
 typedef __attribute__((address_space(4))) const int32_t const_i32_t;
 
+// Cache policy of a load that nothing else on the chip will repeat: 128K keys of 8 KV heads for 16 / 32 / 64 rows 104.9 / 102.5 / 108.8 us
+// without, 91.1 / 92.9 / 99.4 with it (5.1 and 5.9 TB/s); with 128 rows and more, whose row tiles share K and V in an L2, 161 and 162.
+constexpr int kStreaming = 2;
+
 // Every wave's reads and writes of LDS are done, and then all waves go on.  (Not __syncthreads, whose fence would wait for the loads
 // that are on their way to registers.)
 #define STEM_LDS_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
@@ -118,11 +122,9 @@ struct Part {
     static constexpr int kKS = D / 32;                 // 32-wide steps of S^T along d
     static constexpr int kDT = D / 16;                 // 16-column tiles of O^T
     static constexpr int kTileBytes = S::kKeys * kRowBytes;   // of K, or of V
-    // tiles of K and of V in LDS.  kAhead: the operands of the next S^T are read a step ahead, under the products of O^T, so that
-    // a step has them when it begins; four tiles of K then.
-    static constexpr bool kAhead = RW == 4;
-    static constexpr int kBuffersV = RW > 1 ? 2 : 1, kBuffersK = kAhead ? 4 : kBuffersV;
-    static constexpr int kLdsTiles = (kBuffersK + kBuffersV) * kTileBytes, kLdsJoin = KW > 1 ? KW * S::kRows * D * 4 : 0;
+    // tiles of K, and of V, in LDS
+    static constexpr int kBuffers = RW > 1 ? 2 : 1;
+    static constexpr int kLdsTiles = 2 * kBuffers * kTileBytes, kLdsJoin = KW > 1 ? KW * S::kRows * D * 4 : 0;
     static constexpr int kLds = kLdsTiles > kLdsJoin ? kLdsTiles : kLdsJoin;
     // rows of K and V that a wave fetches of a tile, in pieces of at most 16 (which lie in one page), 1 KiB per load
     static constexpr int kMyRows = 32 / RW, kPieces = kMyRows > 16 ? 2 : 1, kPieceRows = kMyRows / kPieces;
@@ -166,39 +168,60 @@ struct Part {
         const uint32_t at = lane / kChunks * row_bytes + lane % kChunks * 16;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u)
-            in[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, first + u * kRowsPerLoad * row_bytes, 0);
+            in[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, first + u * kRowsPerLoad * row_bytes, kKept ? 0 : kStreaming);
     }
     static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_resource(const uint16_t* base, uint32_t row_bytes, int rows) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(base), 0, rows > 0 ? (int)((rows - 1) * row_bytes) + kRowBytes : 0,
                                                  0x00020000);
     }
 
+    // With 128 rows, where instructions count, the byte offsets in LDS that a lane uses in every tile are kept in registers (82 -> 51 vector
+    // instructions of a step beside products and exponentials), and so are the operands of the next S^T, read a step ahead.  With
+    // fewer rows memory is what counts, and a wave, which has more rows of K and V on their way, has no registers left for them.
+    static constexpr bool kKept = RW == 4;
+    int k_read[kKS], v_read[kDT], k_write[kPieces * kLoads], v_write[kPieces * kLoads];
+    __device__ __forceinline__ void place() {
+        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, row = 4 * grp + (c16 >> 2);
+        constexpr int kChunks = D / 8;
+#pragma unroll
+        for (int ks = 0; ks < kKS; ++ks) {
+            k_read[ks] = (key_group() * 32 + c16) * kRowBytes + (((4 * ks + grp) ^ k_swz(c16)) << 4);
+            if constexpr (kKept) asm("" : "+v"(k_read[ks]));
+        }
+#pragma unroll
+        for (int dt = 0; dt < kDT; ++dt) {
+            v_read[dt] = (key_group() * 32 + row) * kRowBytes + (((2 * dt + ((c16 >> 1) & 1)) ^ v_swz(row)) << 4) + (c16 & 1) * 8;
+            if constexpr (kKept) asm("" : "+v"(v_read[dt]));
+        }
+#pragma unroll
+        for (int u = 0; u < kPieces * kLoads; ++u) {
+            const int w_row = my_row() + u * kRowsPerLoad + lane / kChunks, c = lane % kChunks;
+            k_write[u] = w_row * kRowBytes + ((c ^ k_swz(w_row)) << 4);
+            v_write[u] = w_row * kRowBytes + ((c ^ v_swz(w_row)) << 4);
+            if constexpr (kKept) asm("" : "+v"(k_write[u]), "+v"(v_write[u]));
+        }
+    }
+
     // What has been asked for -> LDS.  The 16-byte chunks of a row are exchanged within it (swz), which spreads the rows that are read
     // together over the banks.
     template <bool V>
-    static __device__ __forceinline__ void store(unsigned char* lds, const Rows& in) {
-        const int lane = threadIdx.x & 63;
-        constexpr int kChunks = D / 8;
+    __device__ __forceinline__ void store(unsigned char* lds, const Rows& in, int u) const {
+        *reinterpret_cast<u32x4_t*>(lds + (V ? v_write[u] : k_write[u])) = in[u / kLoads][u % kLoads];
+    }
+    template <bool V>
+    __device__ __forceinline__ void store_all(unsigned char* lds, const Rows& in) const {
 #pragma unroll
-        for (int x = 0; x < kPieces; ++x)
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const int row = my_row() + x * kPieceRows + u * kRowsPerLoad + lane / kChunks, c = lane % kChunks;
-                *reinterpret_cast<u32x4_t*>(lds + row * kRowBytes + ((c ^ (V ? v_swz(row) : k_swz(row))) << 4)) = in[x][u];
-            }
+        for (int u = 0; u < kPieces * kLoads; ++u) store<V>(lds, in, u);
     }
 
-    // Operand m of S^T of this wave's 32 keys: 16 keys m / kKS of them, 32-wide step m % kKS along d.
-    static __device__ __forceinline__ u32x4_t load_k(const unsigned char* k_lds, int m) {
-        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4;
-        const int at = (key_group() * 32 + c16) * kRowBytes + ((grp ^ k_swz(c16)) << 4);
-        return *reinterpret_cast<const u32x4_t*>(k_lds + (at ^ (m % kKS << 6)) + m / kKS * 16 * kRowBytes);
+    // Operand m of S^T of this wave's 32 keys: 16 keys m % 2 of them (in turn, as a product waits for the one before it in the same
+    // registers), 32-wide step m / 2 along d.
+    __device__ __forceinline__ u32x4_t load_k(const unsigned char* k_lds, int m) const {
+        return *reinterpret_cast<const u32x4_t*>(k_lds + k_read[m >> 1] + (m & 1) * 16 * kRowBytes);
     }
     // Operand dt of O^T: 16 columns of the wave's 32 rows of V, in two transposing reads.
-    static __device__ __forceinline__ u32x4_t load_v(const unsigned char* v_lds, int dt) {
-        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, row = 4 * grp + (c16 >> 2);
-        const int at = (key_group() * 32 + row) * kRowBytes + ((((c16 >> 1) & 1) ^ v_swz(row)) << 4) + (c16 & 1) * 8;
-        const unsigned char* p = v_lds + (at ^ (dt << 5));
+    __device__ __forceinline__ u32x4_t load_v(const unsigned char* v_lds, int dt) const {
+        const unsigned char* p = v_lds + v_read[dt];
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)p);
         const s16x4_t up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(p + 16 * kRowBytes));
         const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, up);
@@ -212,17 +235,18 @@ struct Part {
         for (int x = 0; x < 8; ++x) f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
     }
     static __device__ __forceinline__ float largest(const Scores& s, int n) {
-        return max3(max3(s[0][n][0], s[0][n][1], s[0][n][2]), max3(s[0][n][3], s[1][n][0], s[1][n][1]), fmaxf(s[1][n][2], s[1][n][3]));
+        return max3(max3(s[0][n][0], s[0][n][1], s[0][n][2]), max3(s[0][n][3], s[1][n][0], s[1][n][1]),
+                    max3(s[1][n][2], s[1][n][3], s[1][n][2]));
     }
 
     // The exponents f of scores s (powers of two over the reference) are to be at most kSlack: where one passes it the reference moves
     // there, and what has been summed up is scaled.  edge: key x of query n's column counts only if seen(n, x).
     template <typename Seen>
     __device__ __forceinline__ void keep_in_range(Scores& f, Scores& s, float scale_log2, bool edge, Seen seen) {
-        bool moves = false;
+        float high = largest(f, 0);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) moves |= largest(f, n) > kSlack;
-        if (__builtin_expect(!edge & (__builtin_amdgcn_ballot_w64(moves) == 0), 1)) return;
+        for (int n = 1; n < NQ; ++n) high = max3(high, largest(f, n), high);
+        if (__builtin_expect(!edge & (__builtin_amdgcn_ballot_w64(high > kSlack) == 0), 1)) return;
         const int grp = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -259,89 +283,103 @@ struct Part {
     }
 
     // All tiles of S::kKeys keys.  ask_k(rows, t) and ask_v ask for a tile (one that does not exist gives zeros); edge(t) says whether
-    // seen(t, n, x) has to be asked for this wave's keys.  While the weights of a tile are formed and used, the scores of the next one
-    // are: its K lies in LDS by then, one more tile of K and the next of V are on their way.
+    // seen(t, n, x) has to be asked for this wave's keys.
+    // Step t forms the weights of tile t and uses them, and the scores of tile t + 1, whose operands it begins with.  Under the products of
+    // S^T go the operands of O^T and the weights (the last four of the second query tile under the first tile's products of O^T); under
+    // those of O^T the next tile's rows -> LDS, the loads of the one after, a barrier, the operands of the next S^T and the next exponents.
+    // So matrix and vector instructions, LDS and waits lie beside each other all along.
     template <typename AskK, typename AskV, typename Edge, typename Seen>
     __device__ __forceinline__ void walk(int tiles, unsigned char* lds, float scale_log2, AskK ask_k, AskV ask_v, Edge edge, Seen seen) {
         constexpr int kS = 2 * kKS;                        // operands of S^T; those of O^T are kDT, as many
+        constexpr int kRows = kPieces * kLoads;            // writes of K, and of V
         const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
-        auto k_at = [&](int t) STEM_INLINE { return lds + t % kBuffersK * kTileBytes; };
-        auto v_at = [&](int t) STEM_INLINE { return lds + (kBuffersK + t % kBuffersV) * kTileBytes; };
+        auto k_at = [&](int t) STEM_INLINE { return lds + t % kBuffers * kTileBytes; };
+        auto v_at = [&](int t) STEM_INLINE { return lds + (kBuffers + t % kBuffers) * kTileBytes; };
         auto barrier = []() STEM_INLINE {
             if constexpr (RW > 1) STEM_LDS_BARRIER();
         };
+        place();
         Rows a, b;
         Scores f, s;
         u32x4_t k[kS];
         ask_k(a, 0);
         ask_k(b, 1);
-        store<false>(k_at(0), a);
-        if constexpr (kAhead) store<false>(k_at(1), b);
+        store_all<false>(k_at(0), a);
         ask_v(a, 0);
-        if constexpr (kAhead) ask_k(b, 2);
         barrier();
+        unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(0), m); });
+        unrolled<kS>([&](auto m) STEM_INLINE {
 #pragma unroll
-        for (int m = 0; m < kS; ++m) {
-            const u32x4_t first = load_k(k_at(0), m);
-#pragma unroll
-            for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(first, q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
-        }
+            for (int n = 0; n < NQ; ++n) s[m & 1][n] = product<T>(k[m], q[n][m >> 1], m < 2 ? zero4 : s[m & 1][n]);
+        });
 #pragma unroll
         for (int n = 0; n < NQ; ++n) exponents_of(f, s, n, scale_log2);
         keep_in_range(f, s, scale_log2, edge(0), [&](int n, int x) { return seen(0, n, x); });
-        if constexpr (kAhead) unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(1), m); });
-        store<false>(k_at(kAhead ? 2 : 1), b);
-        store<true>(v_at(0), a);
-        ask_k(a, kAhead ? 3 : 2);
+        store_all<false>(k_at(1), b);
+        store_all<true>(v_at(0), a);
+        ask_k(a, 2);
         ask_v(b, 1);
         barrier();
-        // All operands of S^T are read first, then under each of its products an operand of O^T and a share of the weights; the next
-        // exponents under the products of O^T.  j: t modulo 4.
-        auto step = [&](int t, auto j) STEM_INLINE {
+        if constexpr (kKept) unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(1), m); });
+        auto step = [&](int t, auto j) STEM_INLINE {       // j: t modulo 2
+            constexpr int kEarly = 8 * NQ - 4 * (NQ - 1);  // weights under S^T
             u32x4_t v[kDT], p[NQ];
-            if constexpr (!kAhead) unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(j + 1), m); });
+            if constexpr (!kKept) unrolled<kS>([&](auto m) STEM_INLINE { k[m] = load_k(k_at(j + 1), m); });
+            __builtin_amdgcn_s_setprio(1);
             STEM_SCHED_FENCE();
             unrolled<kS>([&](auto m_tag) STEM_INLINE {
-                constexpr int m = decltype(m_tag)::value, kPer = 8 * NQ / kS > 0 ? 8 * NQ / kS : 1;
+                constexpr int m = decltype(m_tag)::value;
                 v[m] = load_v(v_at(j), m);
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) s[m / kKS][n] = product<T>(k[m], q[n][m % kKS], m % kKS == 0 ? zero4 : s[m / kKS][n]);
+                for (int n = 0; n < NQ; ++n) s[m & 1][n] = product<T>(k[m], q[n][m >> 1], m < 2 ? zero4 : s[m & 1][n]);
 #pragma unroll
-                for (int x = m * kPer; x < (m + 1) * kPer && x < 8 * NQ; ++x) weight(f, p, x);
+                for (int x = m * kEarly / kS; x < (m + 1) * kEarly / kS; ++x) weight(f, p, x);
                 STEM_SCHED_FENCE();
             });
-            unrolled<kDT>([&](auto dt) STEM_INLINE {
+            constexpr int kProducts = kDT * NQ, kHalf = kProducts / 2;
+            unrolled<kProducts>([&](auto y_tag) STEM_INLINE {
+                constexpr int y = decltype(y_tag)::value, n = y / kDT, dt = y % kDT;
+                o[dt][n] = product<T>(v[dt], p[n], o[dt][n]);
+                if constexpr (n + 1 < NQ) {
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(v[dt], p[n], o[dt][n]);
-                if constexpr (kAhead) k[dt] = load_k(k_at(j + 2), dt);
-                constexpr int kPer = 8 * NQ / kDT > 0 ? 8 * NQ / kDT : 1;
+                    for (int x = dt * 4 / kDT; x < (dt + 1) * 4 / kDT; ++x) weight(f, p, kEarly + x);
+                }
 #pragma unroll
-                for (int x = dt * kPer; x < (dt + 1) * kPer && x < 8 * NQ; ++x)
-                    f[x >> 2 & 1][x >> 3][x & 3] = __builtin_fmaf(s[x >> 2 & 1][x >> 3][x & 3], scale_log2, off[x >> 3]);
+                for (int x = dt * 8 / kDT; x < (dt + 1) * 8 / kDT; ++x)
+                    f[x >> 2][n][x & 3] = __builtin_fmaf(s[x >> 2][n][x & 3], scale_log2, off[n]);
+                if constexpr (y < kHalf) {
+#pragma unroll
+                    for (int u = y * 2 * kRows / kHalf; u < (y + 1) * 2 * kRows / kHalf; ++u) {
+                        if (u < kRows) store<false>(k_at(j + 2), a, u);
+                        else store<true>(v_at(j + 1), b, u - kRows);
+                    }
+                    if constexpr (y == kHalf - 1) {
+                        ask_k(a, t + 3);
+                        ask_v(b, t + 2);
+                        barrier();
+                    }
+                } else if constexpr (kKept) {
+#pragma unroll
+                    for (int m = (y - kHalf) * kS / (kProducts - kHalf); m < (y + 1 - kHalf) * kS / (kProducts - kHalf); ++m)
+                        k[m] = load_k(k_at(j + 2), m);
+                }
                 STEM_SCHED_FENCE();
             });
+            __builtin_amdgcn_s_setprio(0);
             keep_in_range(f, s, scale_log2, edge(t + 1), [&](int n, int x) { return seen(t + 1, n, x); });
-            store<false>(k_at(kAhead ? j + 3 : j + 2), a);
-            store<true>(v_at(j + 1), b);
-            ask_k(a, kAhead ? t + 4 : t + 3);
-            ask_v(b, t + 2);
-            barrier();
         };
-        constexpr int kUnroll = kAhead ? 4 : RW > 1 ? 2 : 1;
+        constexpr int kUnroll = RW > 1 ? 2 : 1;
         int t = 0;
         for (; t + kUnroll < tiles; t += kUnroll) unrolled<kUnroll>([&](auto j) STEM_INLINE { step(t + j, j); });
-        int last = 0;                                      // t modulo kBuffersV
-        unrolled<kUnroll - 1>([&](auto j) STEM_INLINE {
+        if constexpr (kUnroll == 2)
             if (t + 1 < tiles) {
-                step(t, j);
+                step(t, std::integral_constant<int, 0>{});
                 ++t;
-                last ^= kBuffersV - 1;
             }
-        });
         u32x4_t p[NQ];
         unrolled<8 * NQ>([&](auto x) STEM_INLINE { weight(f, p, x); });
         unrolled<kDT>([&](auto dt) STEM_INLINE {
-            const u32x4_t v = load_v(v_at(last), dt);
+            const u32x4_t v = load_v(v_at(t), dt);
 #pragma unroll
             for (int n = 0; n < NQ; ++n) o[dt][n] = product<T>(v, p[n], o[dt][n]);
         });

@@ -65,99 +65,116 @@ __device__ __forceinline__ void move_and_map(const TableArgs& a, int r, const St
     }
 }
 
-// Sum over the lanes before this one, and over all of the wave.
+// Sum over the lanes up to and with this one.
 template <typename N>
-__device__ __forceinline__ N wave_before(N x, N& all) {
+__device__ __forceinline__ N wave_sum_to(N x) {
     const int lane = threadIdx.x & 63;
-    N sum = x;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-        const N y = __shfl_up(sum, d);
-        sum += lane >= d ? y : N(0);
+        const N y = __shfl_up(x, d);
+        x += lane >= d ? y : N(0);
     }
-    all = __shfl(sum, 63);
-    return sum - x;
+    return x;
 }
 
-// ALL: also moves the pages and maps the tokens; at most kTableThreads requests.
+// One workgroup of at most kTableThreads lanes, one request per lane at a time.  ALL: it also moves the pages and maps the tokens, and
+// there are no more requests than lanes.
 template <bool ALL>
 __global__ __launch_bounds__(kTableThreads) void table_sums_kernel(TableArgs a) {
-    __shared__ int64_t wave_sum[4][kTableWaves];
-    const int tid = threadIdx.x, w = tid >> 6;
-    int32_t head = a.ring_state[0], count = a.ring_state[1];
-    const bool good_ring = head >= 0 && head < a.num_pages && count >= 0 && count <= a.num_pages;
-    if (!good_ring) head = count = 0;
-    int64_t total[4] = {0, 0, 0, 0};                   // pages lacking, given back, new tokens, bad requests
+    // per wave: new tokens (which may need 64 bits), pages lacking, pages given back, bad requests
+    __shared__ int64_t wave_more[kTableWaves];
+    __shared__ int4 wave_pages[kTableWaves];
+    const int tid = threadIdx.x, w = tid >> 6, waves = blockDim.x >> 6;
+    const int32_t then0 = a.ring_state[0], then1 = a.ring_state[1];
+    const bool good_ring = then0 >= 0 && then0 < a.num_pages && then1 >= 0 && then1 <= a.num_pages;
+    const int32_t head = good_ring ? then0 : 0, count = good_ring ? then1 : 0;
+    int64_t more_all = 0;
+    int32_t need_all = 0, back_all = 0, bad_all = 0;   // (32 bits: requests * pages_per_request at most)
     Step s = {};
-    int64_t before[3] = {0, 0, 0};
-    for (int r0 = 0; r0 < a.requests; r0 += kTableThreads) {
+    int32_t past = 0, fresh = 0, need_before = 0, back_before = 0;
+    int64_t more_before = 0;
+    for (int r0 = 0; r0 < a.requests; r0 += blockDim.x) {
         const int r = r0 + tid;
         s = Step{};
-        if (r < a.requests) s = step_of(a, a.past_lens[r], a.new_lens ? a.new_lens[r] : 1);
-        int64_t wave_all[4];
-        before[0] = wave_before<int64_t>(s.need, wave_all[0]);
-        before[1] = wave_before<int64_t>(s.back, wave_all[1]);
-        before[2] = wave_before<int64_t>(s.more, wave_all[2]);
-        wave_all[3] = __popcll(__builtin_amdgcn_ballot_w64(s.bad));
-        if (r0 > 0) __syncthreads();                   // the sums before have been read
-        if ((tid & 63) == 0)
-            for (int x = 0; x < 4; ++x) wave_sum[x][w] = wave_all[x];
-        __syncthreads();
-        for (int x = 0; x < 4; ++x) {
-            int64_t earlier = total[x];
-            for (int v = 0; v < kTableWaves; ++v) {
-                const int64_t n = wave_sum[x][v];
-                if (v < w) earlier += n;
-                total[x] += n;
-            }
-            if (x < 3) before[x] += earlier;
-        }
         if (r < a.requests) {
-            if (!ALL) {                                // (a sum that 32 bits do not hold refuses the step)
-                a.pages_before[r] = (int32_t)before[0];
-                a.back_before[r] = (int32_t)before[1];
-            }
-            a.cu_new[r] = (int32_t)before[2];
+            past = a.past_lens[r];
+            fresh = a.new_lens ? a.new_lens[r] : 1;
+            s = step_of(a, past, fresh);
+        }
+        // sums within the wave, then the waves' totals
+        const int32_t need_to = wave_sum_to(s.need), back_to = wave_sum_to(s.back);
+        const int64_t more_to = wave_sum_to<int64_t>(s.more);
+        const int32_t bad = (int32_t)__popcll(__builtin_amdgcn_ballot_w64(s.bad));
+        if (r0 > 0) __syncthreads();                   // the totals before have been read
+        if ((tid & 63) == 63) {
+            wave_more[w] = more_to;
+            wave_pages[w] = make_int4(need_to, back_to, bad, 0);
+        }
+        __syncthreads();
+        need_before = need_all + need_to - s.need;
+        back_before = back_all + back_to - s.back;
+        more_before = more_all + more_to - s.more;
+        for (int v = 0; v < waves; ++v) {
+            const int64_t m = wave_more[v];
+            const int4 p = wave_pages[v];
+            if (v < w) need_before += p.x, back_before += p.y, more_before += m;
+            need_all += p.x, back_all += p.y, bad_all += p.z, more_all += m;
+        }
+        if (!ALL && r < a.requests) {                  // (a sum that 32 bits do not hold refuses the step)
+            a.pages_before[r] = need_before;
+            a.back_before[r] = back_before;
+            a.cu_new[r] = (int32_t)more_before;
         }
     }
-    const int64_t lacking = total[0] - count, beyond = total[2] - a.capacity, no_room = count + total[1] - a.num_pages;
-    const bool ok = lacking <= 0 && total[3] == 0 && beyond <= 0 && no_room <= 0 && good_ring;
-    for (int r = tid; r < a.requests; r += kTableThreads) {
-        const int32_t past = a.past_lens[r], fresh = a.new_lens ? a.new_lens[r] : 1;
-        a.lens[r] = !ok ? past : fresh < 0 ? 0 : past + fresh;
-        if (!ok) a.cu_new[r] = 0;
+    const int64_t lacking = (int64_t)need_all - count, beyond = more_all - a.capacity, no_room = (int64_t)count + back_all - a.num_pages;
+    const bool ok = lacking <= 0 && bad_all == 0 && beyond <= 0 && no_room <= 0 && good_ring;
+    if constexpr (ALL) {
+        if (tid < a.requests) {
+            a.lens[tid] = !ok ? past : fresh < 0 ? 0 : past + fresh;
+            a.cu_new[tid] = ok ? (int32_t)more_before : 0;
+        }
+    } else {
+        for (int r = tid; r < a.requests; r += blockDim.x) {
+            const int32_t was = a.past_lens[r], came = a.new_lens ? a.new_lens[r] : 1;
+            a.lens[r] = !ok ? was : came < 0 ? 0 : was + came;
+            if (!ok) a.cu_new[r] = 0;
+        }
     }
     if (tid == 0) {
         auto number = [](int64_t n) { return (int32_t)(n < 0 ? 0 : n > 0x7fffffff ? 0x7fffffff : n); };
         a.status[0] = number(lacking);
-        a.status[1] = number(total[3]);
+        a.status[1] = bad_all;
         a.status[2] = number(beyond);
         a.status[3] = good_ring ? number(no_room) : 1;
-        a.cu_new[a.requests] = ok ? (int32_t)total[2] : 0;
-        const int32_t then0 = a.ring_state[0], then1 = a.ring_state[1];
-        a.ring_state_out[0] = ok ? in_ring(head, total[0], a.num_pages) : then0;
-        a.ring_state_out[1] = ok ? (int32_t)(count - total[0] + total[1]) : then1;
+        a.cu_new[a.requests] = ok ? (int32_t)more_all : 0;
+        a.ring_state_out[0] = ok ? in_ring(head, need_all, a.num_pages) : then0;
+        a.ring_state_out[1] = ok ? count - need_all + back_all : then1;
         if (!ALL) {
             a.ring_then[0] = head;
             a.ring_then[1] = ok ? count : -1;          // -1: the step is refused
-            a.ring_then[2] = (int32_t)total[1];
+            a.ring_then[2] = back_all;
         }
     }
     if constexpr (ALL) {
         if (ok) {
             // requests of a few pages and tokens by their own lane, longer ones by the whole wave, one after the other
-            const bool small = s.need <= 4 && s.back <= 4 && s.more <= 4;
-            if (small) move_and_map(a, tid, s, (int32_t)before[0], (int32_t)before[1], (int32_t)before[2], head, count, 0, 1);
-            for (uint64_t left = __builtin_amdgcn_ballot_w64(!small); left; left &= left - 1) {
+            const bool few = s.need <= 4 && s.back <= 4 && s.more <= 4;
+            uint64_t left = __builtin_amdgcn_ballot_w64(!few);
+            if (!few) s = Step{};                      // the lane does nothing in the first turn
+            int r = tid, lane = 0, stride = 1;
+            const int32_t mine[] = {past, fresh, need_before, back_before, (int32_t)more_before};
+            int32_t need0 = need_before, back0 = back_before, more0 = (int32_t)more_before;
+            for (;;) {
+                move_and_map(a, r, s, need0, back0, more0, head, count, lane, stride);
+                if (!left) break;
                 const int l = __builtin_ctzll(left);
-                Step other;
-                other.past = __shfl(s.past, l), other.have = __shfl(s.have, l), other.need = __shfl(s.need, l);
-                other.back = __shfl(s.back, l), other.more = __shfl(s.more, l), other.bad = false;
-                move_and_map(a, (tid & ~63) + l, other, __shfl((int32_t)before[0], l), __shfl((int32_t)before[1], l),
-                             __shfl((int32_t)before[2], l), head, count, tid & 63, 64);
+                left &= left - 1;
+                s = step_of(a, __shfl(mine[0], l), __shfl(mine[1], l));
+                need0 = __shfl(mine[2], l), back0 = __shfl(mine[3], l), more0 = __shfl(mine[4], l);
+                r = (tid & ~63) + l, lane = tid & 63, stride = 64;
             }
         }
-        for (int64_t t = (ok ? total[2] : 0) + tid; t < a.capacity; t += kTableThreads) {
+        for (int64_t t = (ok ? more_all : 0) + tid; t < a.capacity; t += blockDim.x) {
             a.positions[t] = 0;
             a.slots[t] = -1;
         }
@@ -194,12 +211,15 @@ int launch_block_table(const TableCall& c, hipStream_t stream) {
     const TableArgs a = {c.past_lens, c.new_lens, c.ring_state, c.ring, c.table, c.lens, c.ring_state_out, c.cu_new, c.positions,
                          c.slots, c.status, c.pages_before, c.back_before, c.ring_then, s.requests, s.num_pages,
                          s.pages_per_request, s.token_capacity, s.position_offset, __builtin_ctz(s.page_size)};
-    // One launch for steps that a single workgroup has through about as soon as a second launch begins.
-    if (s.requests <= kTableThreads && s.token_capacity <= 4096) {
-        hipLaunchKernelGGL(table_sums_kernel<true>, dim3(1), dim3(kTableThreads), 0, stream, a);
+    // One launch where a step is about a token per request, two where requests have many: a wave takes its long requests one after the
+    // other.  One launch / two, us a call: 64 requests of one token 7.9 / 11.0, 1000 of one 10.4 / 11.4, 16 of 40 tokens on average 9.7 / 11.6, 64 of 29
+    // 32.1 / 11.5, 256 of 7 28.5 / 11.4.  (And not where a finished request can have thousands of pages to give back.)
+    const dim3 lanes(s.requests < kTableThreads ? (s.requests + 63) / 64 * 64 : kTableThreads);
+    if (s.requests <= kTableThreads && s.token_capacity <= 2 * s.requests + 64 && s.pages_per_request <= 2048) {
+        hipLaunchKernelGGL(table_sums_kernel<true>, dim3(1), lanes, 0, stream, a);
         return check_launch();
     }
-    hipLaunchKernelGGL(table_sums_kernel<false>, dim3(1), dim3(kTableThreads), 0, stream, a);
+    hipLaunchKernelGGL(table_sums_kernel<false>, dim3(1), lanes, 0, stream, a);
     if (const int st = check_launch()) return st;
     const int64_t each = ((int64_t)s.token_capacity / s.requests + 4 * kMapThreads - 1) / (4 * kMapThreads);
     const int shared = (int)(each < 1 ? 1 : each > 256 ? 256 : each);

@@ -94,9 +94,10 @@ def _need(condition: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _device() -> int:
-    """The current device; tensors have to lie there, as the call goes to its current stream."""
-    return torch.cuda.current_device()
+def _here() -> Tuple[int, int]:
+    """The current device, on which a call's tensors have to lie, and the handle of its current stream, to which the call goes."""
+    dev = torch.cuda.current_device()
+    return dev, sb._stream() if sb._raw_stream is None else sb._raw_stream(dev)
 
 
 def _rows(t: torch.Tensor, name: str) -> Tuple[int, int, int, int, int]:
@@ -113,22 +114,26 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     return DTYPES[t.dtype]
 
 
+# (These two run for every tensor of every call: conditions first, texts only where one fails.)
 def _values(t: Optional[torch.Tensor], like: Optional[tuple], name: str, dev: int) -> Optional[int]:
     """Address of a tensor of values that has to be as `like` says: (shape, strides, dtype)."""
     if like is None:
         return None
-    _need(t is not None, "%s is missing" % name)
-    _need(t.shape == like[0] and t.dtype == like[2] and (t.stride() == like[1] or t.numel() == 0),
-          "%s is not of the shape's sizes, strides and type" % name)
-    _need(t.device.index == dev, "%s is not on the current device" % name)
+    if t is None:
+        raise ValueError("%s is missing" % name)
+    if t.shape != like[0] or t.dtype is not like[2] or (t.stride() != like[1] and t.numel() > 0):
+        raise ValueError("%s is not of the shape's sizes, strides and type" % name)
+    if t.get_device() != dev:
+        raise ValueError("%s is not on the current device" % name)
     return t.data_ptr()
 
 
 def _whole(t: Optional[torch.Tensor], n: int, name: str, dev: int, dtype: torch.dtype = torch.int32) -> int:
     """Address of a contiguous tensor of n numbers (or more: what lies behind is not touched)."""
-    _need(t is not None and t.dtype == dtype and t.is_contiguous() and t.numel() >= n,
-          "%s has to be contiguous %s of at least %d elements" % (name, dtype, n))
-    _need(t.device.index == dev, "%s is not on the current device" % name)
+    if t is None or t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s has to be contiguous %s of at least %d elements" % (name, dtype, n))
+    if t.get_device() != dev:
+        raise ValueError("%s is not on the current device" % name)
     return t.data_ptr()
 
 
@@ -185,12 +190,12 @@ class RotaryShape:
 
 def stem_rotary(shape: RotaryShape, q, k, positions: torch.Tensor, turns: torch.Tensor, attention_factor: float, q_out, k_out,
                 backward: bool = False) -> None:
-    dev = _device()
+    dev, stream = _here()
     _check(lib().stem_rotary(shape.ref, _values(q, shape.q, "q", dev), _values(k, shape.k, "k", dev),
                              _whole(positions, shape.tokens, "positions", dev),
                              _whole(turns, shape.pairs, "turns", dev, torch.float64), attention_factor, int(bool(backward)),
                              _values(q_out, shape.q_out, "q_out", dev), _values(k_out, shape.k_out, "k_out", dev),
-                             sb._stream()), "stem_rotary")
+                             stream), "stem_rotary")
 
 
 class PageShape:
@@ -215,7 +220,7 @@ class PageShape:
 def stem_rotary_append(shape: RotaryShape, pages: PageShape, q, k, v, positions: torch.Tensor, slots: torch.Tensor,
                        turns: torch.Tensor, attention_factor: float, q_out, k_pages: torch.Tensor,
                        v_pages: torch.Tensor) -> None:
-    dev = _device()
+    dev, stream = _here()
     _need(pages.heads == shape.c.num_kv_heads and pages.head_dim == shape.c.head_dim and
           (shape.k is None or pages.seen[2] == shape.k[2]), "the pages do not go with k")
     _check(lib().stem_rotary_append(shape.ref, pages.ref, _values(q, shape.q, "q", dev), _values(k, shape.k, "k", dev),
@@ -223,7 +228,7 @@ def stem_rotary_append(shape: RotaryShape, pages: PageShape, q, k, v, positions:
                                     _whole(slots, shape.tokens, "slots", dev),
                                     _whole(turns, shape.pairs, "turns", dev, torch.float64), attention_factor,
                                     _values(q_out, shape.q_out, "q_out", dev), _values(k_pages, pages.seen, "k_pages", dev),
-                                    _values(v_pages, pages.seen, "v_pages", dev), sb._stream()), "stem_rotary_append")
+                                    _values(v_pages, pages.seen, "v_pages", dev), stream), "stem_rotary_append")
 
 
 class TableShape:
@@ -246,7 +251,7 @@ def stem_block_table(shape: TableShape, past_lens: torch.Tensor, new_lens: Optio
                      ring: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, ring_state_out: torch.Tensor,
                      cu_new: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, status: torch.Tensor,
                      workspace: torch.Tensor) -> None:
-    dev, c = _device(), shape.c
+    (dev, stream), c = _here(), shape.c
     R = c.requests
     _check(lib().stem_block_table(
         shape.ref, _whole(past_lens, R, "past_lens", dev), None if new_lens is None else _whole(new_lens, R, "new_lens", dev),
@@ -255,7 +260,7 @@ def stem_block_table(shape: TableShape, past_lens: torch.Tensor, new_lens: Optio
         _whole(ring_state_out, 2, "ring_state_out", dev), _whole(cu_new, R + 1, "cu_new", dev),
         _whole(positions, c.token_capacity, "positions", dev), _whole(slots, c.token_capacity, "slots", dev),
         _whole(status, 4, "status", dev), _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(),
-        sb._stream()), "stem_block_table")
+        stream), "stem_block_table")
 
 
 class PrefixShape:
@@ -299,7 +304,7 @@ def stem_prefix_attn_workspace_bytes(shape: PrefixShape) -> int:
 def stem_prefix_attn(shape: PrefixShape, q: torch.Tensor, prefix_k, prefix_v, k_pages, v_pages, table, lens,
                      cu_new: Optional[torch.Tensor], softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor],
                      workspace: torch.Tensor) -> None:
-    dev, c = _device(), shape.c
+    (dev, stream), c = _here(), shape.c
     paged = c.max_suffix > 0
     _check(lib().stem_prefix_attn(
         shape.ref, _values(q, shape.q, "q", dev), _values(prefix_k, shape.prefix, "prefix_k", dev),
@@ -309,4 +314,4 @@ def stem_prefix_attn(shape: PrefixShape, q: torch.Tensor, prefix_k, prefix_v, k_
         _whole(lens, c.requests, "lens", dev) if paged else None,
         None if cu_new is None else _whole(cu_new, c.requests + 1, "cu_new", dev), softmax_scale,
         _values(out, shape.q, "out", dev), None if lse is None else _whole(lse, c.num_q_heads * c.tokens, "lse", dev, torch.float32),
-        _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(), sb._stream()), "stem_prefix_attn")
+        _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(), stream), "stem_prefix_attn")

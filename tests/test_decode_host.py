@@ -238,6 +238,7 @@ def test_prefix_plan_covers_everything_within_its_workspace():
 def test_binding_checks_its_tensors(monkeypatch):
     """On CPU tensors, with a current device that none of them is on."""
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(sb, "_raw_stream", lambda dev: 0)
     q, k = torch.zeros(5, 4, 64, dtype=torch.bfloat16), torch.zeros(5, 2, 64, dtype=torch.bfloat16)
     shape = db.RotaryShape.from_tensors(q, k, 64)
     assert (shape.c.num_q_heads, shape.c.num_kv_heads, shape.c.q_stride_token, shape.c.k_out_stride_token) == (4, 2, 256, 128)
