@@ -1,0 +1,125 @@
+"""Buffer plumbing around include/stem_decode.h: rotary positions, a paged KV cache for what follows a pre-filled prompt, and
+decoding steps of many requests that share it.  No arithmetic here."""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import decode_binding as db
+
+
+class Rotary:
+    """Rotary positions of heads of `head_dim` values, of which the first `rotary_dim` turn (None: all), in the "half" or
+    "interleaved" layout, with frequencies scaled for long contexts by one of decode_binding.SCALINGS."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, theta: float = 10000.0, layout: str = "half",
+                 scaling: str = "none", factor: float = 1.0, trained_length: float = 0.0, low: float = 1.0,
+                 high: float = 4.0, device="cuda"):
+        self.head_dim, self.rotary_dim, self.layout = int(head_dim), int(rotary_dim or head_dim), layout
+        turns, self.attention_factor = db.stem_rotary_frequencies(self.rotary_dim, theta, scaling, factor, trained_length, low, high)
+        self.turns = turns.to(device)
+
+    @classmethod
+    def none(cls, head_dim: int, device="cuda") -> "Rotary":
+        """Positions that turn nothing: keys and queries (of finite values) stay as they are."""
+        r = cls(head_dim, 2, device=device)
+        r.turns.zero_()
+        return r
+
+    def _run(self, q, k, positions, q_out, k_out, backward: bool) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+        q_out = torch.empty_like(q) if q_out is None and q is not None else q_out
+        k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
+        shape = db.RotaryShape.from_tensors(q, k, self.rotary_dim, self.layout, q_out, k_out)
+        db.stem_rotary(shape, q, k, positions, self.turns, self.attention_factor, q_out, k_out, backward)
+        return q_out, k_out
+
+    def apply(self, q, k, positions: torch.Tensor, q_out=None, k_out=None):
+        """q [T, Hq, d] and k [T, Hkv, d] (either may be None) turned by positions int32 [T]; into new tensors unless q_out and
+        k_out are given, which may be q and k themselves."""
+        return self._run(q, k, positions, q_out, k_out, False)
+
+    def backward(self, grad_q, grad_k, positions: torch.Tensor, grad_q_out=None, grad_k_out=None):
+        """The gradients of apply's inputs from those of its outputs."""
+        return self._run(grad_q, grad_k, positions, grad_q_out, grad_k_out, True)
+
+
+class PagedCache:
+    """Keys and values of up to `requests` requests in `num_pages` pages of `page_size` tokens, at most `pages_per_request` each, with the
+    block tables, lengths and free pages that go with them, all on the GPU.  `tokens` is the number of rows of a step's tensors: a step has
+    at most that many new tokens.  `position_offset`: the position of a request's first token (a shared prefix's length)."""
+
+    def __init__(self, requests: int, num_pages: int, page_size: int, pages_per_request: int, num_kv_heads: int, head_dim: int,
+                 tokens: Optional[int] = None, position_offset: int = 0, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        self.requests, self.tokens = int(requests), int(tokens if tokens is not None else requests)
+        self.k_pages, self.v_pages = (torch.empty(num_pages, page_size, num_kv_heads, head_dim, dtype=dtype, device=device)
+                                      for _ in range(2))
+        self.pages = db.PageShape.from_tensors(self.k_pages, self.v_pages)
+        self.shape = db.TableShape(requests, page_size, num_pages, pages_per_request, self.tokens, position_offset)
+        self.max_suffix = int(pages_per_request) * int(page_size)
+
+        def whole(*sizes, value=0):
+            return torch.full(sizes, value, dtype=torch.int32, device=device)
+
+        self.table = whole(self.requests, pages_per_request, value=-1)
+        self.lens, self.cu_new, self.status = whole(self.requests), whole(self.requests + 1), whole(4)
+        self.positions, self.slots = whole(max(self.tokens, 1)), whole(max(self.tokens, 1), value=-1)
+        self.ring = torch.arange(num_pages, dtype=torch.int32, device=device)
+        self.ring_state = torch.tensor([0, num_pages], dtype=torch.int32, device=device)
+        self.workspace = torch.empty(db.stem_block_table_workspace_bytes(self.shape), dtype=torch.uint8, device=device)
+
+    def advance(self, new_lens: Optional[torch.Tensor] = None) -> None:
+        """Room for a step: new_lens int32 [requests] new tokens (None: one each; negative: the request has finished and its pages
+        go back).  Brings lens, table, cu_new, positions and slots up to date; a step for which there is no room changes none of
+        the first two, has no tokens and says so in status (see refused)."""
+        db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
+                            self.cu_new, self.positions, self.slots, self.status, self.workspace)
+
+    def refused(self) -> Tuple[int, int, int, int]:
+        """What the last step lacked: pages; requests with unusable lengths or too long for their row; tokens beyond the step's rows; room
+        for pages given back.  Waits for the GPU."""
+        return tuple(self.status.tolist())
+
+    def append(self, rotary: Rotary, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+               q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """The step's new rows, q [tokens, Hq, d], k and v [tokens, Hkv, d] in the order of the requests: q and k turned, k and v
+        written to the pages.  Rows behind the last new token are left alone."""
+        if q is not None and q_out is None:
+            q_out = torch.empty_like(q)
+        shape = db.RotaryShape.from_tensors(q, k, rotary.rotary_dim, rotary.layout, q_out)
+        db.stem_rotary_append(shape, self.pages, q, k, v, self.positions, self.slots, rotary.turns, rotary.attention_factor, q_out,
+                              self.k_pages, self.v_pages)
+        return q_out
+
+
+class StemDecode:
+    """Decoding steps of the requests of a PagedCache behind a prefix that they share: prefix_k, prefix_v [L, Hkv, d], its keys turned
+    already, as StemPrefill leaves them.  One object is one sequence of steps: its buffers belong to one step at a time.  A step may be
+    captured into a graph and replayed."""
+
+    def __init__(self, prefix_k: torch.Tensor, prefix_v: torch.Tensor, num_q_heads: int, cache: PagedCache,
+                 rotary: Optional[Rotary] = None, max_new: int = 1, softmax_scale: Optional[float] = None,
+                 want_lse: bool = False):
+        d, dev, dtype = prefix_k.shape[2], prefix_k.device, prefix_k.dtype
+        self.prefix_k, self.prefix_v, self.cache = prefix_k, prefix_v, cache
+        self.rotary = rotary if rotary is not None else Rotary.none(d, dev)
+        self.softmax_scale = float(softmax_scale if softmax_scale is not None else d ** -0.5)
+        self.q = torch.zeros(cache.tokens, num_q_heads, d, dtype=dtype, device=dev)      # turned
+        self.out = torch.zeros_like(self.q)
+        self.lse = torch.zeros(num_q_heads, cache.tokens, dtype=torch.float32, device=dev) if want_lse else None
+        self.shape = db.PrefixShape.from_tensors(self.q, prefix_k, cache.pages, cache.table, max_new, cache.max_suffix)
+        self.workspace = torch.empty(db.stem_prefix_attn_workspace_bytes(self.shape), dtype=torch.uint8, device=dev)
+
+    def attend(self) -> torch.Tensor:
+        """Attention of self.q's rows, whose keys and values are in the cache, to the prefix and to their requests' tokens."""
+        c = self.cache
+        db.stem_prefix_attn(self.shape, self.q, self.prefix_k, self.prefix_v, c.k_pages, c.v_pages, c.table, c.lens, c.cu_new,
+                            self.softmax_scale, self.out, self.lse, self.workspace)
+        return self.out
+
+    def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, new_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One step: room for the new tokens, their keys and values into the cache, their attention.  Rows as in PagedCache.append; at most
+        max_new tokens per request.  Returns self.out, whose rows behind the last new token keep what they held."""
+        self.cache.advance(new_lens)
+        self.cache.append(self.rotary, q, k, v, self.q)
+        return self.attend()

@@ -7,6 +7,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import binding as sb
+from .decode import PagedCache, Rotary, StemDecode
 
 
 class StemPrefill:
@@ -15,7 +16,8 @@ class StemPrefill:
     q [T,Hq,d], k and v [Tk,Hkv,d]: bf16 CUDA tensors (k and v with equal strides).  With
     chunk = (starts, ends), q holds only the tokens of each sequence's chunk (T = their sum) while
     k and v keep all Tk = cu_seqlens[-1] rows; pass the same `workspace` to the calls of one
-    prompt so that the pooled keys of earlier chunks are kept.
+    prompt so that the pooled keys of earlier chunks are kept.  With `rotary`, q and k are not yet turned: run() turns them by
+    their positions in their sequences into buffers of its own (self.q, self.k), which the stages use.
     """
 
     def __init__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: Sequence[int],
@@ -23,11 +25,19 @@ class StemPrefill:
                  n_sink: int = 4, n_local: int = 4, beta: float = 0.2, route_scale: float = 1.0,
                  softmax_scale: Optional[float] = None, want_lse: bool = False, ad_stride: int = 1,
                  chunk=None, workspace: Optional[torch.Tensor] = None, group_share: Optional[str] = None,
-                 fill_scores: bool = False):
+                 fill_scores: bool = False, rotary: Optional[Rotary] = None):
         if not (q.is_cuda and k.is_cuda and v.is_cuda):
             raise RuntimeError("StemPrefill needs device tensors; there is no CPU path")
         assert q.dtype == k.dtype == v.dtype == torch.bfloat16
         assert k.stride() == v.stride() and k.shape == v.shape
+        self.rotary = rotary
+        if rotary is not None:
+            if chunk is not None:
+                raise ValueError("a chunk's queries and keys are turned before the call, with Rotary.apply")
+            self.unturned = q, k
+            self.positions = torch.cat([torch.arange(int(hi) - int(lo), dtype=torch.int32)
+                                        for lo, hi in zip(cu_seqlens, cu_seqlens[1:])]).to(q.device)
+            q, k = (torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) for x in (q, k))
         self.q, self.k, self.v = q, k, v
         self.shape = sb.Shape.from_tensors(q, k, block_size, cu_seqlens, chunk)
         self.n_sink, self.n_local = int(n_sink), int(n_local)
@@ -60,6 +70,9 @@ class StemPrefill:
         self.indices = torch.empty((Hl, self.rows, self.kmax), dtype=torch.int32, device=dev)
         self.out = torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device=dev)  # O uses Q's strides
         self.lse = torch.empty((Hq, T), dtype=torch.float32, device=dev) if want_lse else None
+
+    def rotate(self) -> None:
+        self.rotary.apply(*self.unturned, self.positions, self.q, self.k)
 
     def estimate(self) -> None:
         sb.stem_estimate(self.shape, self.q, self.k, self.v, self.beta, self.route_scale,
@@ -99,7 +112,14 @@ class StemPrefill:
                                 self.ad_stride, self.budget, self.n_sink, self.n_local, self.counts,
                                 self.indices, self.kmax, debug_scores, self.workspace)
 
+    def decode(self, cache: PagedCache, sequence: int = 0, max_new: int = 1, want_lse: bool = False) -> StemDecode:
+        """Decoding steps of the cache's requests behind one of the pre-filled sequences, with this layer's rotary positions and scale."""
+        rows = slice(self.shape.cu_seqlens[sequence], self.shape.cu_seqlens[sequence + 1])
+        return StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, self.rotary, max_new, self.softmax_scale, want_lse)
+
     def run(self, fused: bool = False) -> torch.Tensor:
+        if self.rotary is not None:
+            self.rotate()
         if fused:
             self.estimate_select()
         else:

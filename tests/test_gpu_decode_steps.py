@@ -1,0 +1,177 @@
+"""The operators together, as they are used: a prompt turned and pre-filled, then steps of requests that share it (prompts of their
+own, single tokens, drafts, finished requests and new ones in their place), against exact attention over what every request has seen."""
+import pytest
+import torch
+
+from paper_2603_06274_amd.decode import PagedCache, Rotary, StemDecode
+from paper_2603_06274_amd.prefill import StemPrefill
+
+import decode_util as du
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF = torch.bfloat16
+
+
+def rows(g, n, h, d, dtype=BF):
+    return torch.randn(n, h, d, generator=g).to(dtype)
+
+
+class Server:
+    """Requests' keys and values as Python keeps them: turned in 64 bits, rounded once, as the cache's are (to a half step more)."""
+
+    def __init__(self, decode, rotary, prefix, Hq, Hkv, d, R, offset, max_new):
+        self.decode, self.rotary, self.prefix = decode, rotary, prefix
+        self.Hq, self.Hkv, self.d, self.R, self.offset, self.max_new = Hq, Hkv, d, R, offset, max_new
+        self.k, self.v = [[] for _ in range(R)], [[] for _ in range(R)]
+
+    def step(self, g, new):
+        cache, dec = self.decode.cache, self.decode
+        T = cache.tokens
+        q, k, v = rows(g, T, self.Hq, self.d), rows(g, T, self.Hkv, self.d), rows(g, T, self.Hkv, self.d)
+        dec.out.fill_(9.0)
+        out = dec.step(q.to(DEV), k.to(DEV), v.to(DEV), torch.tensor(new, dtype=torch.int32, device=DEV)).cpu()
+        assert cache.refused() == (0, 0, 0, 0)
+        k_pages, v_pages, table, q_turned = cache.k_pages.cpu(), cache.v_pages.cpu(), cache.table.cpu(), dec.q.cpu()
+        t = 0
+        for r, n in enumerate(new):
+            if n < 0:
+                self.k[r], self.v[r] = [], []
+            for i in range(max(n, 0)):
+                pos = torch.tensor([self.offset + len(self.k[r])], dtype=torch.int32)
+                want, bound = du.rotary_reference(k[t + i:t + i + 1], pos, self.rotary.turns.cpu(), 1.0, self.rotary.rotary_dim,
+                                                  self.rotary.layout)
+                place = len(self.k[r])
+                got = k_pages[table[r, place // k_pages.shape[1]], place % k_pages.shape[1]]
+                assert ((got.double() - want[0]).abs() <= bound[0]).all()
+                want, bound = du.rotary_reference(q[t + i:t + i + 1], pos, self.rotary.turns.cpu(), 1.0, self.rotary.rotary_dim,
+                                                  self.rotary.layout)
+                assert ((q_turned[t + i].double() - want[0]).abs() <= bound[0]).all()
+                self.k[r].append(got.double())
+                self.v[r].append(v[t + i].double())
+            # attention, exact over what the cache holds
+            for i in range(max(n, 0)):
+                sees = len(self.k[r]) - n + i + 1
+                ks = torch.cat([self.prefix[0].double(), torch.stack(self.k[r][:sees])]).repeat_interleave(self.Hq // self.Hkv, 1)
+                vs = torch.cat([self.prefix[1].double(), torch.stack(self.v[r][:sees])]).repeat_interleave(self.Hq // self.Hkv, 1)
+                o, bound, _, _ = du.attention_rows(q_turned[t + i].double(), ks, vs, dec.softmax_scale, BF)
+                assert ((out[t + i].double() - o).abs() <= bound).all(), (r, i)
+            t += max(n, 0)
+        assert (out[t:] == 9.0).all()
+        assert cache.lens.tolist() == [len(x) for x in self.k]
+
+
+@pytest.mark.parametrize("d,layout,P", [(128, "half", 16), (64, "interleaved", 64)])
+def test_prompt_then_steps(d, layout, P):
+    g = torch.Generator().manual_seed(d)
+    Hq, Hkv, lens = 8, 2, (300, 517)
+    T = sum(lens)
+    q, k, v = rows(g, T, Hq, d).to(DEV), rows(g, T, Hkv, d).to(DEV), rows(g, T, Hkv, d).to(DEV)
+    rotary = Rotary(d, theta=500000.0, layout=layout, scaling="bands", factor=8.0, trained_length=8192.0)
+    pf = StemPrefill(q, k, v, [0, 300, T], 64, [9, 9], 1.0, n_sink=1, n_local=1, rotary=rotary)
+    out = pf.run().clone()
+    # the same as on queries and keys that were turned before, and those as the formula has them
+    pos = torch.cat([torch.arange(n, dtype=torch.int32) for n in lens])
+    turned = rotary.apply(q, k, pos.to(DEV))
+    for got, x in zip(turned, (q, k)):
+        want, bound = du.rotary_reference(x.cpu(), pos, rotary.turns.cpu(), 1.0, d, layout)
+        assert ((got.cpu().double() - want).abs() <= bound).all()
+    plain = StemPrefill(*turned, v, [0, 300, T], 64, [9, 9], 1.0, n_sink=1, n_local=1)
+    assert torch.equal(out, plain.run()) and torch.equal(pf.k, turned[1])
+    # requests behind the second sequence
+    R = 5
+    cache = PagedCache(R, 40, P, 12, Hkv, d, tokens=40, position_offset=lens[1])
+    cache.k_pages.fill_(float("nan")), cache.v_pages.fill_(float("nan"))
+    dec = pf.decode(cache, sequence=1, max_new=30)
+    server = Server(dec, rotary, (pf.k[300:].cpu(), v[300:].cpu()), Hq, Hkv, d, R, lens[1], 30)
+    for new in ([20, 1, 0, 12, 3], [1, 1, 1, 1, 1], [3, 2, 7, 1, 0], [-1, 1, 1, -1, 1], [30, 0, 1, 9, 0], [1, 1, 1, 1, 1], [-1] * 5,
+                [1, 0, 0, 0, 25]):
+        server.step(g, new)
+
+
+def test_a_step_without_room_changes_nothing():
+    g = torch.Generator().manual_seed(1)
+    Hq, Hkv, d = 4, 1, 64
+    pk, pv = rows(g, 100, Hkv, d).to(DEV), rows(g, 100, Hkv, d).to(DEV)
+    cache = PagedCache(2, 2, 16, 4, Hkv, d, tokens=40, position_offset=100)
+    dec = StemDecode(pk, pv, Hq, cache, max_new=40)
+    args = [rows(g, 40, h, d).to(DEV) for h in (Hq, Hkv, Hkv)]
+    dec.step(*args, torch.tensor([10, 16], dtype=torch.int32, device=DEV))
+    assert cache.refused() == (0, 0, 0, 0)
+    before = [x.clone() for x in (cache.k_pages, cache.v_pages, cache.table, cache.lens, cache.ring_state, dec.out)]
+    dec.step(*[x * 2 for x in args], torch.tensor([1, 1], dtype=torch.int32, device=DEV))
+    assert cache.refused() == (1, 0, 0, 0)
+    for x, y in zip(before, (cache.k_pages, cache.v_pages, cache.table, cache.lens, cache.ring_state, dec.out)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    dec.step(*args, torch.tensor([1, -1], dtype=torch.int32, device=DEV))      # and the next one goes on
+    assert cache.refused() == (0, 0, 0, 0) and cache.lens.tolist() == [11, 0]
+
+
+def test_captured_steps_are_eager_steps():
+    """Two caches that start alike: one steps in a replayed graph, the other eagerly, with other work and waits between."""
+    g = torch.Generator().manual_seed(2)
+    Hq, Hkv, d, R = 8, 2, 128, 6
+    pk, pv = rows(g, 700, Hkv, d).to(DEV), rows(g, 700, Hkv, d).to(DEV)
+    rotary = Rotary(d, theta=10000.0)
+    made = []
+    for _ in range(2):
+        cache = PagedCache(R, 30, 16, 8, Hkv, d, tokens=R + 2, position_offset=700)
+        made.append(StemDecode(pk, pv, Hq, cache, rotary, max_new=3, want_lse=True))
+    a, b = made
+    q, k, v = (torch.zeros(R + 2, h, d, dtype=BF, device=DEV) for h in (Hq, Hkv, Hkv))
+    new = torch.zeros(R, dtype=torch.int32, device=DEV)
+    a.step(q, k, v, new)                               # (no tokens) once before the capture
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step(q, k, v, new)
+    b.step(q, k, v, new)
+    for step in range(12):
+        fresh = [[1] * 6, [3, 0, 1, 1, 0, 2], [-1, 1, 1, 1, 1, 1], [1, 1, -1, 1, 1, 1]][step % 4]
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, generator=g).to(BF))
+        new.copy_(torch.tensor(fresh, dtype=torch.int32))
+        graph.replay()
+        if step % 3 == 0:
+            torch.cuda.synchronize()
+        (q.float() @ q.float().transpose(1, 2)).sum()
+        b.step(q, k, v, new)
+        torch.cuda.synchronize()
+        assert a.cache.refused() == (0, 0, 0, 0)
+        for x, y in ((a.out, b.out), (a.lse, b.lse), (a.cache.table, b.cache.table), (a.cache.lens, b.cache.lens), (a.q, b.q)):
+            assert torch.equal(x, y), step
+
+
+def test_two_decoders_on_two_streams():
+    g = torch.Generator().manual_seed(3)
+    Hq, Hkv, d, R = 8, 2, 64, 4
+    pk, pv = rows(g, 3000, Hkv, d).to(DEV), rows(g, 3000, Hkv, d).to(DEV)
+    rotary = Rotary(d)
+    decoders = [StemDecode(pk, pv, Hq, PagedCache(R, 20, 16, 5, Hkv, d), rotary) for _ in range(3)]
+    inputs = [[rows(g, R, h, d).to(DEV) for h in (Hq, Hkv, Hkv)] for _ in range(8)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    for x in inputs:
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(decoders[i].step(*x).clone())
+    torch.cuda.synchronize()
+    for i, x in enumerate(inputs):
+        want = decoders[2].step(*x)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0][i], want) and torch.equal(outs[1][i], want)
+
+
+def test_rotary_backward_and_none():
+    g = torch.Generator().manual_seed(4)
+    q, k = rows(g, 20, 4, 64, torch.float32).to(DEV), rows(g, 20, 2, 64, torch.float32).to(DEV)
+    pos = torch.arange(20, dtype=torch.int32, device=DEV) * 1000
+    r = Rotary(64, 32, layout="interleaved")
+    back = r.backward(*r.apply(q, k, pos), pos)        # orthogonal: there and back
+    for x, y in zip(back, (q, k)):
+        # two turns, each 9 u (|x1| + |x2|) f off, of values up to sqrt(2) the larger
+        assert ((x - y).abs() <= 9 * du.U * 2 * 1.5 * 2 * y.abs().max()).all()
+    same = Rotary.none(64).apply(q, None, pos)
+    assert torch.equal(same[0], q) and same[1] is None
+    with pytest.raises(ValueError):
+        StemPrefill(*(rows(g, 64, 1, 64).to(DEV) for _ in range(3)), [0, 64], 64, [1], chunk=([0], [64]), rotary=r)
