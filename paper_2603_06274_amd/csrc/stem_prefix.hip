@@ -133,6 +133,7 @@ struct Part {
 
     using Rows = u32x4_t[kPieces][kLoads];             // a wave's rows of K or V, on their way
 
+    bool idle;                                         // no row of the wave's is one
     u32x4_t q[NQ][kKS];
     f32x4_t o[kDT][NQ];
     float off[NQ], l[NQ];                              // minus the reference, in powers of two; sum of the lane's keys
@@ -148,6 +149,7 @@ struct Part {
     // Row m of a KV head is token first + m / G, head m % G of the group; m0 is the workgroup's first.
     __device__ __forceinline__ void load_q(const uint16_t* base, int64_t st, int64_t sh, int first, int G, int m0, int m_end) {
         const int lane = threadIdx.x & 63;
+        idle = m0 + 16 * NQ * row_group() >= m_end;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             const int m = min(m0 + 16 * (NQ * row_group() + n) + (lane & 15), m_end - 1), t = m / G;   // rows past the end repeat the last
@@ -300,6 +302,26 @@ struct Part {
         };
         place();
         Rows a, b;
+        if (RW > 1 && idle) {                              // all of the wave's rows lie behind the last: its share of the loads is all it does
+            ask_k(a, 0);
+            ask_k(b, 1);
+            store_all<false>(k_at(0), a);
+            ask_v(a, 0);
+            barrier();
+            store_all<false>(k_at(1), b);
+            store_all<true>(v_at(0), a);
+            ask_k(a, 2);
+            ask_v(b, 1);
+            barrier();
+            for (int t = 0; t + 1 < tiles; ++t) {
+                store_all<false>(k_at(t + 2), a);
+                store_all<true>(v_at(t + 1), b);
+                ask_k(a, t + 3);
+                ask_v(b, t + 2);
+                barrier();
+            }
+            return;
+        }
         Scores f, s;
         u32x4_t k[kS];
         ask_k(a, 0);
@@ -625,9 +647,10 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
     const bool many = p.prefix_splits + p.suffix_splits > 4;
     const int64_t joined = (int64_t)a.requests * a.max_new * a.Hq, joins = many ? joined : (joined + kGroups - 1) / kGroups;
     if (a.prefix_groups + own_groups > 1 << 22 || joins > 1 << 23) return STEM_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
-    const dim3 grid((unsigned)(a.prefix_groups + own_groups)), block(64 * W);
+    const dim3 grid((unsigned)(a.prefix_groups + own_groups));
     if (grid.x > 0) {
-#define STEM_PREFIX_LAUNCH(SP, SO) hipLaunchKernelGGL((prefix_attn_kernel<T, D, SP, SO>), grid, block, 0, stream, a)
+#define STEM_PREFIX_LAUNCH(SP, SO) \
+    hipLaunchKernelGGL((prefix_attn_kernel<T, D, SP, SO>), grid, dim3(64 * SP::kWaves), 0, stream, a)
         const bool few = p.suffix_row_tile == 16;
         if (p.row_tile == 16) STEM_PREFIX_LAUNCH(Rows16, Rows16);
         else if (p.row_tile == 32 && few) STEM_PREFIX_LAUNCH(Rows32, Rows16);
