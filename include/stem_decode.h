@@ -90,8 +90,8 @@ typedef struct stem_rotary_shape {
  * and y = x for the values from rotary_dim on.  With backward = 1, s is negated: the transposed map, which takes the gradients
  * of y to those of x (and, if attention_factor is 1, the inverse).
  * positions is int32 [tokens] (any sign), turns fp64 [rotary_dim / 2].  q_out may be q and k_out may be k, with the same
- * strides; otherwise an output shares no value with an input or the other output.  STEM_ERR_UNSUPPORTED beyond 2^24 tokens or
- * 65535 heads in all.
+ * strides; otherwise an output shares no value with an input or the other output.  STEM_ERR_UNSUPPORTED from 2^24 tokens or
+ * beyond 65535 heads in all.
  */
 int stem_rotary(const stem_rotary_shape* shape, const void* q, const void* k, const int32_t* positions,
                 const double* turns, float attention_factor, int32_t backward, void* q_out, void* k_out,

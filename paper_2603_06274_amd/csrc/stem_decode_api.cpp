@@ -36,7 +36,7 @@ static int check_rotary(const stem_rotary_shape* s, const void* q, const void* k
     if (!s) return STEM_ERR_INVALID_ARG;
     if (s->dtype != STEM_BF16 && s->dtype != STEM_FP16 && s->dtype != STEM_FP32) return STEM_ERR_INVALID_ARG;
     if (s->tokens < 0 || s->num_q_heads < 0 || s->num_kv_heads < 0) return STEM_ERR_INVALID_ARG;
-    if (s->tokens > 1 << 24 || (int64_t)s->num_q_heads + 2 * (int64_t)s->num_kv_heads > 65535) return STEM_ERR_UNSUPPORTED;
+    if (s->tokens >= 1 << 24 || (int64_t)s->num_q_heads + 2 * (int64_t)s->num_kv_heads > 65535) return STEM_ERR_UNSUPPORTED;
     if (s->num_q_heads + s->num_kv_heads == 0 || s->head_dim <= 0 || s->head_dim % 8) return STEM_ERR_INVALID_ARG;
     if (s->head_dim > STEM_MAX_HEAD_DIM) return STEM_ERR_UNSUPPORTED;
     if (s->rotary_dim < 2 || s->rotary_dim % 2 || s->rotary_dim > s->head_dim) return STEM_ERR_INVALID_ARG;

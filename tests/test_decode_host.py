@@ -88,7 +88,7 @@ def rotary(c, q=P, k=P, pos=P, turns=P, factor=1.0, backward=0, q_out=P, k_out=P
 
 
 def test_rotary_refusals():
-    for kw, status in ((dict(dtype=3), BAD), (dict(tokens=-1), BAD), (dict(tokens=(1 << 24) + 1), NO),
+    for kw, status in ((dict(dtype=3), BAD), (dict(tokens=-1), BAD), (dict(tokens=(1 << 24) + 1), NO), (dict(tokens=1 << 24), NO),
                        (dict(num_q_heads=-1), BAD), (dict(num_q_heads=0, num_kv_heads=0), BAD), (dict(num_q_heads=70000), NO),
                        (dict(head_dim=0), BAD), (dict(head_dim=100), BAD), (dict(head_dim=2048), NO),
                        (dict(rotary_dim=0), BAD), (dict(rotary_dim=63), BAD), (dict(rotary_dim=130), BAD), (dict(layout=2), BAD),

@@ -128,9 +128,10 @@ def test_sums_beyond_32_bits_refuse():
     assert cu.tolist() == [0] * (R + 1) and slots.tolist() == [-1] * 100 and (table == -7).all() and lens.tolist() == [0] * R
 
 
-def test_replays_go_on():
+@pytest.mark.parametrize("cap", [25, 700])             # one launch, two launches
+def test_replays_go_on(cap):
     """A captured step, replayed with the books kept in place, beside eager steps of other books."""
-    b, c = Books(20, 16, 6, 100, 25, seed=3), Books(20, 16, 6, 100, 25, seed=3)
+    b, c = Books(20, 16, 6, 100, cap, seed=3), Books(20, 16, 6, 100, cap, seed=3)
     new = torch.ones(20, dtype=torch.int32, device=DEV)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):

@@ -274,6 +274,24 @@ def test_replays_follow_lengths_and_tables():
         assert torch.equal(out, eager) and torch.equal(z, z2)
 
 
+@pytest.mark.parametrize("Hq,d", [(1, 64), (4, 128), (24, 128), (60, 64), (130, 128), (40, 256)])
+@pytest.mark.parametrize("L", [1, 5, 17, 31, 65, 100, 129, 700])
+def test_nothing_behind_the_prefix_is_read(Hq, d, L):
+    """The prefix as the first rows of a longer tensor whose other rows are NaN, at every row tile, in one part and in several."""
+    g = torch.Generator().manual_seed(L)
+    q = torch.randn(2, Hq, d, generator=g).to(BF)
+    k, v = (torch.full((L + 900, 1, d), float("nan"), dtype=BF) for _ in range(2))
+    k[:L], v[:L] = (torch.randn(L, 1, d, generator=g).to(BF) for _ in range(2))
+    dq, dk, dv = q.to(DEV), k.to(DEV), v.to(DEV)
+    shape = db.PrefixShape.from_tensors(dq, dk[:L], None, 2, 1, 0)
+    space = torch.empty(db.stem_prefix_attn_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(dq)
+    db.stem_prefix_attn(shape, dq, dk[:L], dv[:L], None, None, None, None, None, d ** -0.5, out, None, space)
+    for t in range(2):
+        o, bound, _, _ = du.attention_rows(q[t].double(), *(x[:L].double().expand(L, Hq, d) for x in (k, v)), d ** -0.5, BF)
+        assert ((out[t].cpu().double() - o).abs() <= bound).all()
+
+
 def test_workspace_too_small():
     c = Case([5], [1], 10)
     q, pk = c.q.to(DEV), c.pk.to(DEV)
