@@ -147,6 +147,13 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
         p.suffix_splits = (int32_t)(wanted < tiles ? wanted : tiles);
         if (p.suffix_splits > 64) p.suffix_splits = 64;
     }
+    // A second launch costs about 3 us: that is what a workgroup takes for the tiles that it would have shared with others.  One launch / two, us a
+    // call of 8 requests: d = 64, 8 / 2 heads, 300 keys 8.2 / 11.1, 1000 9.3 / 11.1, 1500 10.5 / 11.1, 2000 11.8 / 11.2; d = 128, 32 / 8 heads, 240 keys 9.4 /
+    // 11.1, 1040 14.5 / 11.5; d = 256, 140 keys 13.4 / 15.3 and for one request 13.6 / 10.9.  (The prefix within 32-bit byte offsets, too.)
+    const int64_t most_small = s.head_dim == 64 ? 1536 : s.head_dim == 128 ? 384 : -1;
+    p.small = own_rows <= 16 && (int64_t)s.requests * s.num_kv_heads <= units_here && (int64_t)s.prefix_len + s.max_suffix <= most_small &&
+              (s.prefix_len == 0 || ((int64_t)s.prefix_len + 127) / 128 * 128 * s.prefix_stride_token * 2 <= kInt32Max);
+    if (p.small) p.prefix_splits = p.suffix_splits = 0;
     const int64_t parts = (int64_t)(p.prefix_splits + p.suffix_splits) * s.num_kv_heads * rows;
     p.partial_ml = align256(sizeof(float) * (size_t)parts * s.head_dim);
     p.bytes = p.partial_ml + align256(2 * sizeof(float) * (size_t)parts);

@@ -48,6 +48,7 @@ struct PrefixPlan {
     int32_t suffix_row_tile;
     int32_t suffix_row_tiles;  // per request: ceil(max_new * G / suffix_row_tile)
     int32_t suffix_splits;     // 0 if there are no pages
+    bool small;                // all of a request's keys by one workgroup per KV head, no parts
     size_t partial_ml;         // byte offset in the workspace: (maximum, sum) of every partial result
     size_t bytes;
 };

@@ -107,6 +107,19 @@ constexpr int kStreaming = 2;
 // that are on their way to registers.)
 #define STEM_LDS_BARRIER() asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory")
 
+// Four values of a row's output from their sums, and (with the first four) its lse.
+template <typename T>
+__device__ __forceinline__ void write_row(const PrefixArgs& a, int token, int head, int at, f32x4_t o, float l, float m) {
+    const bool empty = l == 0.f;
+    const float inv = empty ? 0.f : 1.f / l;
+    uint2 packed;
+    packed.x = pack<T>(o[0] * inv, o[1] * inv);
+    packed.y = pack<T>(o[2] * inv, o[3] * inv);
+    reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + (int64_t)token * a.q_st + (int64_t)head * a.q_sh)[at] = packed;
+    if (a.lse && at == 0)
+        a.lse[(int64_t)head * a.tokens + token] = empty ? -__builtin_huge_valf() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 // How the waves of a workgroup share its rows and keys: RW groups of 16 NQ rows times KW groups of 32 keys.  With RW = 1 every wave has
 // keys of its own and waits for no other; with RW > 1 the tile of 32 KW keys in LDS is read by RW waves each, and there are two
 // of them in turn, with a barrier per tile.
@@ -407,6 +420,46 @@ struct Part {
         });
     }
 
+    // The waves' results together -> the rows' outputs, where there are no other parts.  Row m0 of m_end is row m0 of token `first`.
+    __device__ __forceinline__ void finish_rows(unsigned char* lds, float2* wave_ml, const PrefixArgs& a, int first, int g, int m0, int m_end) {
+        const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+            if (grp == 0) wave_ml[kw * S::kRows + row0 + 16 * n + c16] = make_float2(-off[n], l[n]);
+        }
+        __syncthreads();                               // every wave is done with its tiles
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            const int row = row0 + 16 * n + c16;
+            float m = wave_ml[row].x;
+#pragma unroll
+            for (int v = 1; v < KW; ++v) m = fmaxf(m, wave_ml[v * S::kRows + row].x);
+            const float mine = __builtin_amdgcn_exp2f(-off[n] - m);
+            float* dst = reinterpret_cast<float*>(lds) + (kw * S::kRows + row) * D + 4 * grp;
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[dt][n] * mine;
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < S::kRows * D / 4; x += 64 * kWaves) {
+            const int row = x / (D / 4), at = x % (D / 4);
+            if (m0 + row >= m_end) break;
+            float m = wave_ml[row].x, sum = 0.f;
+#pragma unroll
+            for (int v = 1; v < KW; ++v) m = fmaxf(m, wave_ml[v * S::kRows + row].x);
+            f32x4_t all = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < KW; ++v) {
+                const float2 ml = wave_ml[v * S::kRows + row];
+                sum += ml.y * __builtin_amdgcn_exp2f(ml.x - m);
+                all += reinterpret_cast<const f32x4_t*>(lds)[v * S::kRows * D / 4 + x];
+            }
+            const int t = (m0 + row) / a.G;
+            write_row<T>(a, first + t, g * a.G + m0 + row - t * a.G, at, all, sum, m);
+        }
+    }
+
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
     __device__ __forceinline__ void finish(unsigned char* lds, float2* wave_ml, float* part, float2* ml, int m0, int m_end) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
@@ -461,6 +514,65 @@ struct Part {
     }
 };
 
+// The prefix's keys key0 .. key0 + keys - 1 of KV head g.
+template <typename S, typename P>
+__device__ __forceinline__ void walk_prefix(P& t, const PrefixArgs& a, int g, int key0, int keys, unsigned char* lds) {
+    const uint16_t* k = a.prefix_k + (int64_t)key0 * a.p_st + g * a.p_sh;
+    const uint16_t* v = a.prefix_v + (int64_t)key0 * a.p_st + g * a.p_sh;
+    const uint32_t row_bytes = (uint32_t)a.p_st * 2;
+    const auto rk = P::rows_resource(k, row_bytes, keys), rv = P::rows_resource(v, row_bytes, keys);
+    const int tiles = (keys + S::kKeys - 1) / S::kKeys;
+    auto ask = [&](typename P::Rows& rows, __amdgpu_buffer_rsrc_t rsrc, int tile) STEM_INLINE {
+        // behind the last tile there is nothing (and its offset is within 32 bits, which those further on need not be)
+        const uint32_t first = (uint32_t)(min(tile, tiles) * S::kKeys + t.my_row()) * row_bytes;
+#pragma unroll
+        for (int x = 0; x < P::kPieces; ++x) t.fetch(rows[x], rsrc, row_bytes, first + x * P::kPieceRows * row_bytes);
+    };
+    const int left = keys - t.key_group() * 32;        // of this wave's keys in tile 0
+    t.walk(
+        tiles, lds, a.scale_log2, [&](auto& rows, int tile) STEM_INLINE { ask(rows, rk, tile); },
+        [&](auto& rows, int tile) STEM_INLINE { ask(rows, rv, tile); }, [&](int tile) { return left - tile * S::kKeys < 32; },
+        [&](int tile, int, int x) { return x < left - tile * S::kKeys; });
+}
+
+// Keys key0 .. key0 + keys - 1 of request r's `len` own, for rows m0 .. of its m_end (new tokens times heads of the group); n new tokens.
+template <typename S, typename P>
+__device__ __forceinline__ void walk_own(P& t, const PrefixArgs& a, int r, int g, int n, int len, int key0, int keys, int m0, int m_end,
+                                         unsigned char* lds) {
+    const int lane = threadIdx.x & 63;
+    // keys of this part that the lane's columns see: those up to the token itself
+    int sees[S::NQ];
+#pragma unroll
+    for (int x = 0; x < S::NQ; ++x)
+        sees[x] = len - key0 - n + min(m0 + 16 * (S::NQ * t.row_group() + x) + (lane & 15), m_end - 1) / a.G + 1;
+    const int least = min(len - key0 - n + m0 / a.G + 1, keys);   // of the workgroup's rows
+    const_i32_t* row = (const_i32_t*)(a.table + (int64_t)r * a.table_row);
+    const int mask = (1 << a.page_shift) - 1;
+    auto page_of = [&](int key) {                      // -1: no key of this part, or no page of the cache's
+        const int page = key < keys ? __builtin_amdgcn_readfirstlane(row[(key0 + key) >> a.page_shift]) : -1;
+        return (uint32_t)page < (uint32_t)a.num_pages ? page : -1;
+    };
+    const uint32_t row_bytes = (uint32_t)a.tok_st * 2;
+    auto ask = [&](typename P::Rows& rows, const uint16_t* pages, int tile) STEM_INLINE {
+#pragma unroll
+        for (int x = 0; x < P::kPieces; ++x) {
+            const int key = tile * S::kKeys + t.my_row() + x * P::kPieceRows, page = page_of(key);
+            const int64_t at_key = page < 0 ? 0 : (int64_t)page * a.page_st + (int64_t)((key0 + key) & mask) * a.tok_st + g * a.head_st;
+            t.fetch(rows[x], P::rows_resource(pages + at_key, row_bytes, page < 0 ? 0 : min(keys - key, P::kPieceRows)), row_bytes, 0);
+        }
+    };
+    bool lo = false, hi = false;                       // whether the halves of the wave's 32 keys are in a page
+    t.walk(
+        (keys + S::kKeys - 1) / S::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) STEM_INLINE { ask(rows, a.k_pages, tile); },
+        [&](auto& rows, int tile) STEM_INLINE { ask(rows, a.v_pages, tile); },
+        [&](int tile) {
+            const int key = tile * S::kKeys + t.key_group() * 32;
+            lo = page_of(key) >= 0, hi = page_of(key + 16) >= 0;
+            return !lo || !hi || key + 32 > least;
+        },
+        [&](int tile, int nq, int x) { return tile * S::kKeys + t.key_group() * 32 + x < sees[nq] && (x < 16 ? lo : hi); });
+}
+
 // SP: how the rows of the prefix are shared, SO: those of a request and its own keys.
 template <typename T, int D, typename SP, typename SO>
 __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn_kernel(PrefixArgs a) {
@@ -477,23 +589,8 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
         const int g = combo % a.Hkv, split = combo / a.Hkv, m0 = row_tile * SP::kRows;
         PartP t;
         t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, 0, a.G, m0, a.rows);
-        const int key0 = split * a.split_keys, keys = min(a.split_keys, a.prefix_len - key0);
-        const uint16_t* k = a.prefix_k + (int64_t)key0 * a.p_st + g * a.p_sh;
-        const uint16_t* v = a.prefix_v + (int64_t)key0 * a.p_st + g * a.p_sh;
-        const uint32_t row_bytes = (uint32_t)a.p_st * 2;
-        const auto rk = PartP::rows_resource(k, row_bytes, keys), rv = PartP::rows_resource(v, row_bytes, keys);
-        const int tiles = (keys + SP::kKeys - 1) / SP::kKeys;
-        auto ask = [&](typename PartP::Rows& rows, __amdgpu_buffer_rsrc_t rsrc, int tile) STEM_INLINE {
-            // behind the last tile there is nothing (and its offset is within 32 bits, which those further on need not be)
-            const uint32_t first = (uint32_t)(min(tile, tiles) * SP::kKeys + t.my_row()) * row_bytes;
-#pragma unroll
-            for (int x = 0; x < PartP::kPieces; ++x) t.fetch(rows[x], rsrc, row_bytes, first + x * PartP::kPieceRows * row_bytes);
-        };
-        const int left = keys - t.key_group() * 32;    // of this wave's keys in tile 0
-        t.walk(
-            tiles, lds, a.scale_log2, [&](auto& rows, int tile) STEM_INLINE { ask(rows, rk, tile); },
-            [&](auto& rows, int tile) STEM_INLINE { ask(rows, rv, tile); }, [&](int tile) { return left - tile * SP::kKeys < 32; },
-            [&](int tile, int, int x) { return x < left - tile * SP::kKeys; });
+        const int key0 = split * a.split_keys;
+        walk_prefix<SP>(t, a, g, key0, min(a.split_keys, a.prefix_len - key0), lds);
         const int64_t place = ((int64_t)split * a.Hkv + g) * a.rows;
         t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
         return;
@@ -514,40 +611,28 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     if (keys <= 0) return;
     PartO t;
     t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, m0, mine);
-    const int lane = threadIdx.x & 63;
-    // keys of this part that the lane's columns see: those up to the token itself
-    int sees[SO::NQ];
-#pragma unroll
-    for (int x = 0; x < SO::NQ; ++x)
-        sees[x] = len - key0 - n + min(m0 + 16 * (SO::NQ * t.row_group() + x) + (lane & 15), mine - 1) / a.G + 1;
-    const int least = min(len - key0 - n + m0 / a.G + 1, keys);   // of the workgroup's rows
-    const_i32_t* row = (const_i32_t*)(a.table + (int64_t)r * a.table_row);
-    const int mask = (1 << a.page_shift) - 1;
-    auto page_of = [&](int key) {                      // -1: no key of this part, or no page of the cache's
-        const int page = key < keys ? __builtin_amdgcn_readfirstlane(row[(key0 + key) >> a.page_shift]) : -1;
-        return (uint32_t)page < (uint32_t)a.num_pages ? page : -1;
-    };
-    const uint32_t row_bytes = (uint32_t)a.tok_st * 2;
-    auto ask = [&](typename PartO::Rows& rows, const uint16_t* pages, int tile) STEM_INLINE {
-#pragma unroll
-        for (int x = 0; x < PartO::kPieces; ++x) {
-            const int key = tile * SO::kKeys + t.my_row() + x * PartO::kPieceRows, page = page_of(key);
-            const int64_t at_key = page < 0 ? 0 : (int64_t)page * a.page_st + (int64_t)((key0 + key) & mask) * a.tok_st + g * a.head_st;
-            t.fetch(rows[x], PartO::rows_resource(pages + at_key, row_bytes, page < 0 ? 0 : min(keys - key, PartO::kPieceRows)), row_bytes, 0);
-        }
-    };
-    bool lo = false, hi = false;                       // whether the halves of the wave's 32 keys are in a page
-    t.walk(
-        (keys + SO::kKeys - 1) / SO::kKeys, lds, a.scale_log2, [&](auto& rows, int tile) STEM_INLINE { ask(rows, a.k_pages, tile); },
-        [&](auto& rows, int tile) STEM_INLINE { ask(rows, a.v_pages, tile); },
-        [&](int tile) {
-            const int key = tile * SO::kKeys + t.key_group() * 32;
-            lo = page_of(key) >= 0, hi = page_of(key + 16) >= 0;
-            return !lo || !hi || key + 32 > least;
-        },
-        [&](int tile, int nq, int x) { return tile * SO::kKeys + t.key_group() * 32 + x < sees[nq] && (x < 16 ? lo : hi); });
+    walk_own<SO>(t, a, r, g, n, len, key0, keys, m0, mine, lds);
     const int64_t place = ((int64_t)(a.prefix_splits + split) * a.Hkv + g) * a.rows + (int64_t)first * a.G;
     t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
+}
+
+// Small calls in one launch: a workgroup has all keys of its request's rows, the prefix's (which are read once per request then) and its own.
+template <typename T, int D, typename S>
+__global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a) {
+    using P = Part<T, D, S>;
+    __shared__ __align__(1024) unsigned char lds[P::kLds];
+    __shared__ float2 wave_ml[S::kRows * S::KW];
+    const int g = blockIdx.x % a.Hkv, r = blockIdx.x / a.Hkv;
+    int first, n;
+    new_tokens(a, r, first, n);
+    const int mine = min(n, a.max_new) * a.G;
+    if (mine <= 0) return;
+    P t;
+    t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, 0, mine);
+    if (a.prefix_len > 0) walk_prefix<S>(t, a, g, 0, a.prefix_len, lds);
+    const int len = suffix_len(a, r);
+    if (len > 0) walk_own<S>(t, a, r, g, n, len, 0, len, 0, mine, lds);
+    t.finish_rows(lds, wave_ml, a, first, g, 0, mine);
 }
 
 // Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
@@ -623,15 +708,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         m = top;
     }
     if (i >= n) return;                                // (n is 0 behind the last request)
-    const bool empty = l == 0.f;
-    const float inv = empty ? 0.f : 1.f / l;
-    uint2 packed;
-    packed.x = pack<T>(o[0] * inv, o[1] * inv);
-    packed.y = pack<T>(o[2] * inv, o[3] * inv);
-    uint16_t* out = static_cast<uint16_t*>(a.out) + (int64_t)(first + i) * a.q_st + (int64_t)h * a.q_sh;
-    reinterpret_cast<uint2*>(out)[lane] = packed;
-    if (a.lse && lane == 0)
-        a.lse[(int64_t)h * a.tokens + first + i] = empty ? -__builtin_huge_valf() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    write_row<T>(a, first + i, h, lane, o, l, m);
 }
 
 template <typename T, int D>
@@ -641,6 +718,12 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
     using Rows32 = Split<1, 2, W / 2>;
     using Rows64 = Split<2, 2, W / 2>;
     using Rows128 = Split<2, 4, W / 4>;
+    if constexpr (D != 256)
+        if (p.small) {
+            using Small = Split<1, 1, D == 64 ? 8 : 4>;
+            hipLaunchKernelGGL((small_attn_kernel<T, D, Small>), dim3((unsigned)(a.requests * a.Hkv)), dim3(64 * Small::kWaves), 0, stream, a);
+            return check_launch();
+        }
     const int64_t own_groups = p.suffix_splits > 0 ? (int64_t)a.requests * a.Hkv * p.suffix_row_tiles * p.suffix_splits : 0;
     // several groups of lanes per row where there are parts for them
     constexpr int kGroups = 4 * kJoinThreads / D;

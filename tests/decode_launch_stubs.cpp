@@ -19,7 +19,7 @@ extern "C" int stem_test_prefix_plan(const stem_prefix_shape* shape, int32_t uni
     const int st = stem::prefix_plan(*shape, &p, give_units);
     if (st != STEM_OK) return st;
     const int64_t all[] = {p.row_tile, p.row_tiles, p.prefix_splits, p.split_keys, p.suffix_row_tile, p.suffix_row_tiles,
-                           p.suffix_splits, (int64_t)p.partial_ml, (int64_t)p.bytes};
-    for (int i = 0; i < 9; ++i) out[i] = all[i];
+                           p.suffix_splits, (int64_t)p.partial_ml, (int64_t)p.bytes, p.small};
+    for (int i = 0; i < 10; ++i) out[i] = all[i];
     return STEM_OK;
 }

@@ -208,7 +208,7 @@ def test_prefix_refusals():
 @pytest.mark.skipif(not hasattr(ctypes.CDLL(sb.library_path()), "stem_test_prefix_plan"), reason="needs the host-only build")
 def test_prefix_plan_covers_everything_within_its_workspace():
     L = ctypes.CDLL(sb.library_path())
-    out = (ctypes.c_int64 * 9)()
+    out = (ctypes.c_int64 * 10)()
     some = [1, 2, 3, 7, 16, 17, 33, 64, 100, 1000, 30000]
     for d in (64, 128, 256):
         for hq, hkv in ((1, 1), (32, 8), (28, 4), (8, 1), (64, 1)):
@@ -221,10 +221,13 @@ def test_prefix_plan_covers_everything_within_its_workspace():
                                      pages=pages(stride_page=16 * hkv * d, stride_token=hkv * d, stride_head=d))
                     for units in (256, 304, 32):
                         assert L.stem_test_prefix_plan(ctypes.byref(c), units, out) == sb.STEM_OK
-                        tile, tiles, splits, keys, own, owns, parts, ml, size = list(out)
+                        tile, tiles, splits, keys, own, owns, parts, ml, size, small = list(out)
                         rows = tokens * (hq // hkv)
                         assert tile * (tiles - 1) < rows <= tile * tiles
                         assert own * (owns - 1) < min(7 * (hq // hkv), rows) <= own * owns      # no request has more rows than there are
+                        if small:                      # one workgroup per request and KV head, without parts
+                            assert splits == parts == 0 and owns == 1 and own == 16 and size >= 16
+                            continue
                         if L_:
                             assert keys % 32 == 0 and keys * (splits - 1) < L_ <= keys * splits
                         else:
