@@ -117,8 +117,8 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     p.row_tiles = (int32_t)((rows + p.row_tile - 1) / p.row_tile);
     p.prefix_splits = p.split_keys = 0;
     if (s.prefix_len > 0 && rows > 0) {
-        // Parts of whole tiles, one to four rounds of workgroups (one runs on a CU at a time): whichever ends first, where a part costs
-        // its tiles and about two more to begin and end.
+        // Parts of whole tiles, one to four rounds of workgroups (two run on a CU at a time, one with head size 256): whichever ends first,
+        // where a part costs its tiles and about two more to begin and end.
         const int64_t others = (int64_t)p.row_tiles * s.num_kv_heads;
         const int32_t waves = 4, row_groups = p.row_tile == 16 ? 1 : p.row_tile == 128 ? 4 : 2;
         const int64_t tile = 32 * waves / row_groups, tiles = (s.prefix_len + tile - 1) / tile;

@@ -95,7 +95,10 @@ __device__ __forceinline__ int suffix_len(const PrefixArgs& a, int r) {
 }
 
 constexpr float kNone = -3e38f;                        // reference of a row that has met no key: below any score, and finite
-constexpr float kSlack = 8.f;                          // how far (in powers of two) scores may pass the reference before it moves
+// A reference moves to where the largest weight is 2^lift, when one passes 2^(lift + 8).  In fp16 weights begin to lose bits below 2^-14: a
+// lift of 7 keeps those down to 2^-21 of the largest whole, and 2^15 is within the type.
+template <typename T> constexpr float kLift = std::is_same_v<T, _Float16> ? 7.f : 0.f;
+template <typename T> constexpr float kMost = kLift<T> + 8.f;
 
 typedef __attribute__((address_space(4))) const int32_t const_i32_t;
 
@@ -254,14 +257,14 @@ struct Part {
                     max3(s[1][n][2], s[1][n][3], s[1][n][2]));
     }
 
-    // The exponents f of scores s (powers of two over the reference) are to be at most kSlack: where one passes it the reference moves
-    // there, and what has been summed up is scaled.  edge: key x of query n's column counts only if seen(n, x).
+    // The exponents f of scores s (powers of two over the reference) are to be at most kMost: where one passes it the reference moves,
+    // and what has been summed up is scaled.  edge: key x of query n's column counts only if seen(n, x).
     template <typename Seen>
     __device__ __forceinline__ void keep_in_range(Scores& f, Scores& s, float scale_log2, bool edge, Seen seen) {
         float high = largest(f, 0);
 #pragma unroll
         for (int n = 1; n < NQ; ++n) high = max3(high, largest(f, n), high);
-        if (__builtin_expect(!edge & (__builtin_amdgcn_ballot_w64(high > kSlack) == 0), 1)) return;
+        if (__builtin_expect(!edge & (__builtin_amdgcn_ballot_w64(high > kMost<T>) == 0), 1)) return;
         const int grp = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -274,9 +277,9 @@ struct Part {
             float raw = largest(s, n);
             raw = fmaxf(raw, __shfl_xor(raw, 16));
             raw = fmaxf(raw, __shfl_xor(raw, 32));      // the same in the column's four lanes
-            if (__builtin_fmaf(raw, scale_log2, off[n]) > kSlack) {
+            if (__builtin_fmaf(raw, scale_log2, off[n]) > kMost<T>) {
                 const float then = off[n];
-                off[n] = -raw * scale_log2;
+                off[n] = __builtin_fmaf(-raw, scale_log2, kLift<T>);
                 const float corr = __builtin_amdgcn_exp2f(off[n] - then);
                 l[n] *= corr;
 #pragma unroll

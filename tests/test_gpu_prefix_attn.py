@@ -301,3 +301,21 @@ def test_workspace_too_small():
     with pytest.raises(db.sb.StemError) as e:
         db.stem_prefix_attn(shape, q, pk, pk, None, None, None, None, None, c.scale, torch.empty_like(q), None, space)
     assert e.value.status == db.sb.STEM_ERR_WORKSPACE
+
+
+def test_many_small_weights_beside_a_large_one():
+    """fp16: one key holds half of a row's weight, 60000 others the rest, each with 2^-17 of it, where fp16 has subnormals only.  Their
+    values are alike in sign, so that a loss of small weights would show: it is within 2^-11 of the sum, as of any other."""
+    L, d = 60000, 64
+    g = torch.Generator().manual_seed(5)
+    q = torch.zeros(1, 4, d, dtype=HF)
+    q[:, :, 0] = 8.0
+    k = (0.01 * torch.randn(L, 1, d, generator=g)).to(HF)
+    v = (1.0 + 0.1 * torch.rand(L, 1, d, generator=g)).to(HF)
+    k[0, 0, 0], v[0] = math.log(L), 0.0                # score ln(L) at scale 1/8, the others about 0
+    shape = db.PrefixShape.from_tensors(q.to(DEV), k.to(DEV), None, 1, 1, 0)
+    space = torch.empty(db.stem_prefix_attn_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    out = torch.empty(1, 4, d, dtype=HF, device=DEV)
+    db.stem_prefix_attn(shape, q.to(DEV), k.to(DEV), v.to(DEV), None, None, None, None, None, 0.125, out, None, space)
+    o, _, _, _ = du.attention_rows(q[0].double(), k.double().expand(L, 4, d), v.double().expand(L, 4, d), 0.125, HF)
+    assert ((out[0].cpu().double() - o).abs() <= 2 * 2.0 ** -11 * o.abs()).all()   # weights' rounding and the output's
