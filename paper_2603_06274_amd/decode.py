@@ -84,6 +84,8 @@ class PagedCache:
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """The step's new rows, q [tokens, Hq, d], k and v [tokens, Hkv, d] in the order of the requests: q and k turned, k and v
         written to the pages.  Rows behind the last new token are left alone."""
+        if k.shape[0] != self.tokens:
+            raise ValueError("a step's tensors have %d rows here, as many as the cache was made for" % self.tokens)
         if q is not None and q_out is None:
             q_out = torch.empty_like(q)
         shape = db.RotaryShape.from_tensors(q, k, rotary.rotary_dim, rotary.layout, q_out)

@@ -162,6 +162,19 @@ def test_two_decoders_on_two_streams():
         assert torch.equal(outs[0][i], want) and torch.equal(outs[1][i], want)
 
 
+def test_rows_that_do_not_go_with_the_cache_are_refused():
+    g = torch.Generator().manual_seed(6)
+    pk = rows(g, 50, 1, 64).to(DEV)
+    dec = StemDecode(pk, pk, 4, PagedCache(2, 4, 16, 2, 1, 64, tokens=8))
+    for n in (7, 9):                                   # fewer rows than a step may have tokens, and more
+        with pytest.raises(ValueError):
+            dec.step(*(rows(g, n, h, 64).to(DEV) for h in (4, 1, 1)))
+    with pytest.raises(ValueError):
+        dec.step(*(rows(g, 8, h, 64, torch.float16).to(DEV) for h in (4, 1, 1)))
+    with pytest.raises(ValueError):
+        dec.step(*(rows(g, 8, h, 64).to(DEV) for h in (4, 1, 1)), torch.zeros(2, dtype=torch.int64, device=DEV))
+
+
 def test_rotary_backward_and_none():
     g = torch.Generator().manual_seed(4)
     q, k = rows(g, 20, 4, 64, torch.float32).to(DEV), rows(g, 20, 2, 64, torch.float32).to(DEV)
