@@ -16,7 +16,7 @@ class Rotary:
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, theta: float = 10000.0, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, trained_length: float = 0.0, low: float = 1.0,
                  high: float = 4.0, device="cuda"):
-        self.head_dim, self.rotary_dim, self.layout = int(head_dim), int(rotary_dim or head_dim), layout
+        self.head_dim, self.rotary_dim, self.layout = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), layout
         turns, self.attention_factor = db.stem_rotary_frequencies(self.rotary_dim, theta, scaling, factor, trained_length, low, high)
         self.turns = turns.to(device)
 
@@ -27,10 +27,16 @@ class Rotary:
         r.turns.zero_()
         return r
 
+    def _shape(self, q, k, q_out, k_out=None) -> db.RotaryShape:
+        shape = db.RotaryShape.from_tensors(q, k, self.rotary_dim, self.layout, q_out, k_out)
+        if shape.c.head_dim != self.head_dim:
+            raise ValueError("heads of %d values, and positions made for %d" % (shape.c.head_dim, self.head_dim))
+        return shape
+
     def _run(self, q, k, positions, q_out, k_out, backward: bool) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
         q_out = torch.empty_like(q) if q_out is None and q is not None else q_out
         k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
-        shape = db.RotaryShape.from_tensors(q, k, self.rotary_dim, self.layout, q_out, k_out)
+        shape = self._shape(q, k, q_out, k_out)
         db.stem_rotary(shape, q, k, positions, self.turns, self.attention_factor, q_out, k_out, backward)
         return q_out, k_out
 
@@ -80,18 +86,31 @@ class PagedCache:
         for pages given back.  Waits for the GPU."""
         return tuple(self.status.tolist())
 
+    def _rows_shape(self, rotary: Rotary, q, k, v, q_out) -> db.RotaryShape:
+        """The shape of a step's rows.  Raises unless they go with the cache and with each other."""
+        if k.shape[0] != self.tokens:
+            raise ValueError("a step's tensors have %d rows here, as many as the cache was made for" % self.tokens)
+        shape = rotary._shape(q, k, q_out)
+        if k.dtype != self.k_pages.dtype or k.shape[1:] != self.k_pages.shape[2:]:
+            raise ValueError("k does not go with the cache's pages")
+        if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise ValueError("v has to be of k's sizes, strides and type")
+        if any(t is not None and t.device != self.k_pages.device for t in (q, k, v, q_out)):
+            raise ValueError("a step's tensors have to be on the cache's device")
+        return shape
+
     def append(self, rotary: Rotary, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """The step's new rows, q [tokens, Hq, d], k and v [tokens, Hkv, d] in the order of the requests: q and k turned, k and v
         written to the pages.  Rows behind the last new token are left alone."""
-        if k.shape[0] != self.tokens:
-            raise ValueError("a step's tensors have %d rows here, as many as the cache was made for" % self.tokens)
         if q is not None and q_out is None:
             q_out = torch.empty_like(q)
-        shape = db.RotaryShape.from_tensors(q, k, rotary.rotary_dim, rotary.layout, q_out)
+        self._write(self._rows_shape(rotary, q, k, v, q_out), rotary, q, k, v, q_out)
+        return q_out
+
+    def _write(self, shape: db.RotaryShape, rotary: Rotary, q, k, v, q_out) -> None:
         db.stem_rotary_append(shape, self.pages, q, k, v, self.positions, self.slots, rotary.turns, rotary.attention_factor, q_out,
                               self.k_pages, self.v_pages)
-        return q_out
 
 
 class StemDecode:
@@ -105,6 +124,8 @@ class StemDecode:
         d, dev, dtype = prefix_k.shape[2], prefix_k.device, prefix_k.dtype
         self.prefix_k, self.prefix_v, self.cache = prefix_k, prefix_v, cache
         self.rotary = rotary if rotary is not None else Rotary.none(d, dev)
+        if self.rotary.head_dim != d:
+            raise ValueError("heads of %d values, and positions made for %d" % (d, self.rotary.head_dim))
         self.softmax_scale = float(softmax_scale if softmax_scale is not None else d ** -0.5)
         self.q = torch.zeros(cache.tokens, num_q_heads, d, dtype=dtype, device=dev)      # turned
         self.out = torch.zeros_like(self.q)
@@ -122,6 +143,7 @@ class StemDecode:
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, new_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One step: room for the new tokens, their keys and values into the cache, their attention.  Rows as in PagedCache.append; at most
         max_new tokens per request.  Returns self.out, whose rows behind the last new token keep what they held."""
+        shape = self.cache._rows_shape(self.rotary, q, k, v, self.q)      # (what it refuses leaves the cache as it was)
         self.cache.advance(new_lens)
-        self.cache.append(self.rotary, q, k, v, self.q)
+        self.cache._write(shape, self.rotary, q, k, v, self.q)
         return self.attend()

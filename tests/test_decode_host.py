@@ -10,6 +10,7 @@ import torch
 
 from paper_2603_06274_amd import binding as sb
 from paper_2603_06274_amd import decode_binding as db
+from paper_2603_06274_amd.decode import Rotary
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 BAD, NO, SPACE = sb.STEM_ERR_INVALID_ARG, sb.STEM_ERR_UNSUPPORTED, sb.STEM_ERR_WORKSPACE
@@ -85,6 +86,15 @@ def rotary_shape(**kw):
 
 def rotary(c, q=P, k=P, pos=P, turns=P, factor=1.0, backward=0, q_out=P, k_out=P):
     return db.lib().stem_rotary(ctypes.byref(c) if c is not None else None, q, k, pos, turns, factor, backward, q_out, k_out, None)
+
+
+def test_rotary_of_no_values_is_refused():
+    for wrong in (0, 63):
+        with pytest.raises(sb.StemError):
+            Rotary(64, wrong, device="cpu")
+    assert Rotary(64, device="cpu").rotary_dim == 64
+    with pytest.raises(ValueError):                    # positions of other heads than those that come
+        Rotary(128, device="cpu").apply(torch.zeros(3, 2, 64, dtype=torch.bfloat16), None, torch.zeros(3, dtype=torch.int32))
 
 
 def test_rotary_refusals():

@@ -175,6 +175,28 @@ def test_rows_that_do_not_go_with_the_cache_are_refused():
         dec.step(*(rows(g, 8, h, 64).to(DEV) for h in (4, 1, 1)), torch.zeros(2, dtype=torch.int64, device=DEV))
 
 
+def test_a_refused_step_leaves_the_cache_as_it_was():
+    g = torch.Generator().manual_seed(7)
+    pk = rows(g, 50, 1, 64).to(DEV)
+    cache = PagedCache(2, 4, 16, 2, 1, 64)
+    dec = StemDecode(pk, pk, 4, cache)
+    q, k, v = (rows(g, 2, h, 64).to(DEV) for h in (4, 1, 1))
+    wrong = [(q[:1], k, v), (q[:, :2], k, v), (q, k[:1], v), (q, k.half(), v), (q, k, v[:1]), (q, k, v.half()), (q, k, v.cpu()),
+             (q.cpu(), k, v), (q, torch.cat([k, k], 1), torch.cat([v, v], 1)), (q, k, torch.cat([v, v], 2)[:, :, :64])]
+    for given in wrong:
+        with pytest.raises(ValueError):
+            dec.step(*given)
+    assert cache.lens.tolist() == [0, 0] and cache.ring_state.tolist() == [0, 4]
+    first = dec.step(q, k, v).clone()
+    assert cache.lens.tolist() == [1, 1]
+    again = StemDecode(pk, pk, 4, PagedCache(2, 4, 16, 2, 1, 64))
+    assert torch.equal(first, again.step(q, k, v))
+    with pytest.raises(ValueError):
+        StemDecode(pk, pk, 4, cache, Rotary(128))
+    with pytest.raises(ValueError):
+        Rotary(128).apply(q, None, cache.positions)
+
+
 def test_rotary_backward_and_none():
     g = torch.Generator().manual_seed(4)
     q, k = rows(g, 20, 4, 64, torch.float32).to(DEV), rows(g, 20, 2, 64, torch.float32).to(DEV)
