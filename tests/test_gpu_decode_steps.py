@@ -197,6 +197,22 @@ def test_a_refused_step_leaves_the_cache_as_it_was():
         Rotary(128).apply(q, None, cache.positions)
 
 
+def test_decode_behind_a_sequence_that_is_none_or_of_another_length():
+    g = torch.Generator().manual_seed(8)
+    q, k, v = (rows(g, 400, h, 64).to(DEV) for h in (4, 1, 1))
+    with_rotary, without = (StemPrefill(q, k, v, [0, 150, 400], 64, [3, 4], 1.0, n_sink=1, n_local=1, rotary=r)
+                            for r in (Rotary(64), None))
+    cache = PagedCache(2, 4, 16, 2, 1, 64, position_offset=250)
+    for pf in (with_rotary, without):
+        for sequence in (-1, 2):
+            with pytest.raises(ValueError):
+                pf.decode(cache, sequence)
+        assert pf.decode(cache, 1).shape.c.prefix_len == 250
+    with pytest.raises(ValueError):
+        with_rotary.decode(cache, 0)
+    assert without.decode(cache, 0).shape.c.prefix_len == 150      # (whose positions nothing turns by)
+
+
 def test_rotary_backward_and_none():
     g = torch.Generator().manual_seed(4)
     q, k = rows(g, 20, 4, 64, torch.float32).to(DEV), rows(g, 20, 2, 64, torch.float32).to(DEV)
