@@ -158,7 +158,8 @@ typedef struct stem_prefix_shape {
     int32_t tokens;                  /* rows of Q, O; >= 0                                               */
     int32_t max_new;                 /* most new tokens of a request, >= 1                               */
     int32_t prefix_len;              /* >= 0                                                             */
-    int32_t max_suffix;              /* most tokens that a request has in its pages, 0 .. pages_per_request * page_size */
+    int32_t max_suffix;              /* most tokens that a request has in its pages, 0 .. pages_per_request * page_size,
+                                        and at most 2^31 - 2^14 (beyond: STEM_ERR_UNSUPPORTED)           */
     int32_t pages_per_request;       /* entries of a table row                                           */
     int64_t q_stride_token, q_stride_head;          /* of Q and O                                        */
     int64_t prefix_stride_token, prefix_stride_head;/* of prefix_k and prefix_v                          */

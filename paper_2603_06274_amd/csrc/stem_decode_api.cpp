@@ -97,6 +97,7 @@ static int check_prefix(const stem_prefix_shape* s) {
         if (s->prefix_stride_token > most_prefix) return STEM_ERR_UNSUPPORTED;
     }
     if (s->max_suffix > 0) {
+        if (s->max_suffix > kMaxSuffix) return STEM_ERR_UNSUPPORTED;
         if (const int st = check_pages(s->pages, s->head_dim)) return st;
         if (s->pages.stride_token > most) return STEM_ERR_UNSUPPORTED;
         if (s->pages_per_request < 1) return STEM_ERR_INVALID_ARG;
@@ -143,7 +144,7 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     if (s.max_suffix > 0 && rows > 0) {
         const int64_t others = (int64_t)s.requests * s.num_kv_heads * p.suffix_row_tiles;
         const int64_t wanted = (units_here + others - 1) / others;   // (half as many as fit at a time: 52.0, twice as many 53.9 us with 32K keys)
-        const int64_t tiles = (s.max_suffix + 255) / 256;
+        const int64_t tiles = ((int64_t)s.max_suffix + 255) / 256;
         p.suffix_splits = (int32_t)(wanted < tiles ? wanted : tiles);
         if (p.suffix_splits > 64) p.suffix_splits = 64;
     }

@@ -67,6 +67,10 @@ struct PrefixCall {
 };
 int launch_prefix_attn(const PrefixCall& call, hipStream_t stream);
 
+// Most own tokens of a request.  The kernel counts keys in 32 bits: parts are rounded up to 128 keys and there are 64 at most, and a
+// walk looks three tiles of at most 256 keys past its last one, so that nothing that it forms passes 2^31.
+constexpr int32_t kMaxSuffix = 0x7fffffff - 0x3fff;
+
 // Keys of a part of a request's own `len`, of which there are at most `splits`: whole 128s, so that short ones use few parts.  The
 // kernel that computes partial results and the one that joins them both ask here.
 __host__ __device__ inline int suffix_split_keys(int len, int splits) {
