@@ -174,8 +174,10 @@ int stem_prefix_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* hos
  * over the prefix_len rows of prefix_k, prefix_v [prefix_len, Hkv, d] and the request's rows j in the pages with
  * j <= lens[r] - n + i, where t is number i of the n new tokens of request r (which stand at the end of its lens[r] tokens).
  *   - lens is int32 [requests], table int32 [requests, pages_per_request], cu_new int32 [requests + 1]: request r's new tokens are
- *     the rows cu_new[r] .. cu_new[r + 1] - 1 of Q and O, as far as there are such rows (none if there are none between; a row that a
- *     cu_new which descends gives to two requests holds nothing defined).  cu_new NULL: one token each, then tokens = requests.  Rows of no request are left as they were, in O and in lse, and so are a request's rows from max_new on.
+ *     the rows cu_new[r] .. cu_new[r + 1] - 1 of Q and O, as far as there are such rows.  cu_new ascends (where it does not, rows of
+ *     O and lse hold nothing defined); NULL: one token each, then tokens = requests.  Rows of no request are left as they were, in O
+ *     and in lse, and so are a request's rows from max_new on.  max_new may be as large as a request's tokens can get: the work goes
+ *     by the rows that there are.
  *   - lens outside 0 .. max_suffix count as the nearer of the two.  Rows in pages that are not the cache's (a table entry outside
  *     0 .. num_pages - 1) contribute nothing, and nothing is read there; nor is anything behind a request's last token.
  *   - A row that sees no key at all gives zeros, lse -inf.
@@ -186,7 +188,9 @@ int stem_prefix_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* hos
  *   - The same inputs give the same bits; what the rest of the batch holds has no influence on a row beyond rounding.
  * workspace: 16-byte aligned, of stem_prefix_attn_workspace_bytes (which depends on the current device), this call's alone until its work has
  * finished.  prefix_k and prefix_v may be NULL if prefix_len is 0; k_pages, v_pages, table and lens if max_suffix is 0.
- * STEM_ERR_UNSUPPORTED if 16 rows of a page or 128 of the prefix span 2 GiB or more.
+ * STEM_ERR_UNSUPPORTED, from both functions, if 16 rows of a page or 128 of the prefix span 2 GiB or more, if tokens * num_q_heads or
+ * max_new * num_q_heads exceeds 2^31 - 1, or if a launch would have about 2^31 workgroups (tokens * num_q_heads beyond
+ * 2^31 - 2^20, or requests * num_kv_heads that are as many).
  */
 int stem_prefix_attn(const stem_prefix_shape* shape, const void* q, const void* prefix_k, const void* prefix_v,
                      const void* k_pages, const void* v_pages, const int32_t* table, const int32_t* lens,

@@ -8,6 +8,7 @@
 namespace stem {
 
 constexpr int64_t kInt32Max = 0x7fffffff;
+constexpr int64_t kMostGroups = kInt32Max - (1 << 20);   // of a launch, whose grid is rounded up to lines of 2^20
 
 static bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -140,9 +141,16 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     const int64_t own_rows = s.max_new * G < rows ? s.max_new * G : rows;
     p.suffix_row_tile = own_rows <= 16 ? 16 : 64;
     p.suffix_row_tiles = (int32_t)((own_rows + p.suffix_row_tile - 1) / p.suffix_row_tile);
+    // By the rows that there are, not by what each request might have: max_new is a bound for the longest (a step that takes a prompt of 2048
+    // tokens beside 63 single ones has 131072 row tiles of 64 by the one count, 2175 by the other).
+    const int64_t by_request = (int64_t)s.requests * p.suffix_row_tiles, by_rows = slot_before(s.requests, rows, p.suffix_row_tile);
+    p.own_by_rows = by_request > by_rows;
+    p.own_slots = p.own_by_rows ? by_rows : by_request;
+    p.join_by_rows = (int64_t)s.requests * s.max_new > s.tokens;
+    p.join_rows = (p.join_by_rows ? s.tokens : (int64_t)s.requests * s.max_new) * s.num_q_heads;
     p.suffix_splits = 0;
     if (s.max_suffix > 0 && rows > 0) {
-        const int64_t others = (int64_t)s.requests * s.num_kv_heads * p.suffix_row_tiles;
+        const int64_t others = p.own_slots * s.num_kv_heads;
         const int64_t wanted = (units_here + others - 1) / others;   // (half as many as fit at a time: 52.0, twice as many 53.9 us with 32K keys)
         const int64_t tiles = ((int64_t)s.max_suffix + 255) / 256;
         p.suffix_splits = (int32_t)(wanted < tiles ? wanted : tiles);
@@ -155,6 +163,9 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     p.small = own_rows <= 16 && (int64_t)s.requests * s.num_kv_heads <= units_here && (int64_t)s.prefix_len + s.max_suffix <= most_small &&
               (s.prefix_len == 0 || ((int64_t)s.prefix_len + 127) / 128 * 128 * s.prefix_stride_token * 2 <= kInt32Max);
     if (p.small) p.prefix_splits = p.suffix_splits = 0;
+    p.prefix_groups = ((int64_t)s.num_kv_heads * p.prefix_splits + 7) / 8 * 8 * p.row_tiles;
+    p.groups = p.prefix_groups + p.own_slots * s.num_kv_heads * p.suffix_splits;
+    if (p.groups > kMostGroups || p.join_rows > kMostGroups) return STEM_ERR_UNSUPPORTED;
     const int64_t parts = (int64_t)(p.prefix_splits + p.suffix_splits) * s.num_kv_heads * rows;
     p.partial_ml = align256(sizeof(float) * (size_t)parts * s.head_dim);
     p.bytes = p.partial_ml + align256(2 * sizeof(float) * (size_t)parts);

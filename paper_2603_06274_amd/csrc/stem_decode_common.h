@@ -48,6 +48,14 @@ struct PrefixPlan {
     int32_t suffix_row_tile;
     int32_t suffix_row_tiles;  // per request: ceil(max_new * G / suffix_row_tile)
     int32_t suffix_splits;     // 0 if there are no pages
+    // Pairs (request, row tile) per KV head and part of the own keys: suffix_row_tiles for every request or, where that is more,
+    // rows / tile for all together and one for each (own_by_rows: slot_before says whose a slot is).
+    int64_t own_slots;
+    bool own_by_rows;
+    // Rows (token, head) that are joined: max_new tokens of every request or, where that is more, the call's tokens (join_by_rows).
+    int64_t join_rows;
+    bool join_by_rows;
+    int64_t prefix_groups, groups;   // workgroups of the prefix, and with those of the own keys
     bool small;                // all of a request's keys by one workgroup per KV head, no parts
     size_t partial_ml;         // byte offset in the workspace: (maximum, sum) of every partial result
     size_t bytes;
@@ -70,6 +78,10 @@ int launch_prefix_attn(const PrefixCall& call, hipStream_t stream);
 // Most own tokens of a request.  The kernel counts keys in 32 bits: parts are rounded up to 128 keys and there are 64 at most, and a
 // walk looks three tiles of at most 256 keys past its last one, so that nothing that it forms passes 2^31.
 constexpr int32_t kMaxSuffix = 0x7fffffff - 0x3fff;
+
+// Row tiles' slots before those of request r, whose first row is `row`: whole tiles before the row and one for each request
+// before, which is at least as many as these have tiles.  (floor(b / t) + 1 - floor(a / t) is whole and more than (b - a) / t.)
+__host__ __device__ inline int64_t slot_before(int r, int64_t row, int tile) { return row / tile + r; }
 
 // Keys of a part of a request's own `len`, of which there are at most `splits`: whole 128s, so that short ones use few parts.  The
 // kernel that computes partial results and the one that joins them both ask here.

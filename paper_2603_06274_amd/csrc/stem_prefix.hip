@@ -75,10 +75,13 @@ struct PrefixArgs {
     int32_t prefix_len, split_keys, prefix_splits, row_tiles;
     int32_t max_suffix, suffix_splits, suffix_row_tiles;
     int32_t table_row, page_shift, num_pages;
-    int32_t prefix_groups;                             // workgroups of the prefix
+    int32_t prefix_groups, groups;                     // workgroups of the prefix, and with those of the own keys
+    bool own_by_rows, join_by_rows;                    // how the latter, and the rows that are joined, are counted: PrefixPlan
     int64_t q_st, q_sh, p_st, p_sh, page_st, tok_st, head_st;
 };
 
+// First row of request r's new tokens, within the call's tokens.
+__device__ __forceinline__ int first_token(const PrefixArgs& a, int r) { return a.cu_new ? min(max(a.cu_new[r], 0), a.tokens) : r; }
 // New tokens of request r: the first and their number, within the call's tokens.
 __device__ __forceinline__ void new_tokens(const PrefixArgs& a, int r, int& first, int& n) {
     if (a.cu_new) {
@@ -90,6 +93,25 @@ __device__ __forceinline__ void new_tokens(const PrefixArgs& a, int r, int& firs
         n = 1;
     }
 }
+// The last of 0 .. count - 1 whose key is at most x, -1 if there is none; keys ascend.  The whole wave looks for one x, 64 keys at a time:
+// one load for 64 requests, three for 65536, instead of one after the other.
+template <typename Key>
+__device__ __forceinline__ int last_at_most(int count, int64_t x, Key key) {
+    const int lane = threadIdx.x & 63;
+    int from = 0;
+    while (count > 64) {
+        const int step = (count + 63) / 64, i = lane * step;
+        const uint64_t below = __builtin_amdgcn_ballot_w64(i < count && key(from + i) <= x);
+        if (!below) return -1;
+        const int at = (63 - __builtin_clzll(below)) * step;
+        from += at;
+        count = min(step, count - at);
+    }
+    const uint64_t below = __builtin_amdgcn_ballot_w64(lane < count && key(from + lane) <= x);
+    return below ? from + 63 - __builtin_clzll(below) : -1;
+}
+// A launch's workgroups are numbered along lines of a grid that has more than one if there are very many.
+__device__ __forceinline__ int64_t group_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 __device__ __forceinline__ int suffix_len(const PrefixArgs& a, int r) {
     return a.max_suffix > 0 ? min(max(a.lens[r], 0), a.max_suffix) : 0;
 }
@@ -584,7 +606,9 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     using PartO = Part<T, D, SO>;
     __shared__ __align__(1024) unsigned char lds[PartP::kLds > PartO::kLds ? PartP::kLds : PartO::kLds];
     __shared__ float2 wave_ml[SP::kRows * SP::KW > SO::kRows * SO::KW ? SP::kRows * SP::KW : SO::kRows * SO::KW];
-    const int id = blockIdx.x;
+    const int64_t number = group_number();
+    if (number >= a.groups) return;
+    const int id = (int)number;
     if (id < a.prefix_groups) {
         // row tiles of the same keys on one XCD (workgroup id modulo 8), one after the other: they share its L2
         const int x = id & 7, y = id >> 3, row_tile = y % a.row_tiles, combo = y / a.row_tiles * 8 + x;
@@ -602,13 +626,22 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     int at = id - a.prefix_groups;
     const int g = at % a.Hkv;
     at /= a.Hkv;
-    const int row_tile = at % a.suffix_row_tiles;
-    at /= a.suffix_row_tiles;
-    const int split = at % a.suffix_splits, r = at / a.suffix_splits;
+    const int split = at % a.suffix_splits, slot = at / a.suffix_splits;
+    int r, row_tile;
+    if (a.own_by_rows) {
+        auto before = [&](int x) { return slot_before(x, (int64_t)first_token(a, x) * a.G, SO::kRows); };
+        r = last_at_most(a.requests, slot, before);
+        if (r < 0) return;
+        row_tile = slot - (int)before(r);
+    } else {
+        r = slot / a.suffix_row_tiles;
+        row_tile = slot - r * a.suffix_row_tiles;
+    }
     int first, n;
     new_tokens(a, r, first, n);
-    const int mine = min(n, a.max_new) * a.G, m0 = row_tile * SO::kRows;
-    if (m0 >= mine) return;
+    const int mine = min(n, a.max_new) * a.G;
+    if ((int64_t)row_tile * SO::kRows >= mine) return;
+    const int m0 = row_tile * SO::kRows;
     const int len = suffix_len(a, r);
     const int split_keys = suffix_split_keys(len, a.suffix_splits), key0 = split * split_keys, keys = min(len - key0, split_keys);
     if (keys <= 0) return;
@@ -647,19 +680,43 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
     __shared__ f32x4_t group_o[GROUPS > 1 ? kJoinThreads : 1];
     __shared__ float2 group_ml[GROUPS > 1 ? kRows * GROUPS : 1];
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes % GROUPS, my_row = threadIdx.x / (kLanes * GROUPS);
-    const int64_t item = (int64_t)blockIdx.x * kRows + my_row;   // request, new token, head
-    const int per_request = a.max_new * a.Hq;
-    const int r = (int)(item / per_request), rest = (int)(item - (int64_t)r * per_request), i = rest / a.Hq, h = rest - i * a.Hq, g = h / a.G;
-    int first = 0, n = 0, parts = 0;
-    if (r < a.requests) {
-        new_tokens(a, r, first, n);
-        if (i < n) {
-            const int len = suffix_len(a, r);
-            parts = a.prefix_splits;
-            if (len > 0) {
-                const int each = suffix_split_keys(len, a.suffix_splits);
-                parts += (len + each - 1) / each;
-            }
+    const int64_t item = group_number() * kRows + my_row;
+    int r = 0, i = 0, h = 0, first = 0, n = 0, parts = 0;
+    bool mine = false;                                 // whether the row is one of a request's
+    if (a.join_by_rows) {                              // token, head
+        constexpr int kWaveRows = GROUPS > 1 ? 1 : 64 / kLanes;   // different rows of a wave
+        const int64_t item0 = GROUPS > 1 ? item : group_number() * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
+        int known = -1, owner = -1;
+#pragma unroll
+        for (int x = 0; x < kWaveRows; ++x) {
+            const int64_t token = (item0 + x) / a.Hq;
+            if (token >= a.tokens) break;
+            if (token != known) owner = last_at_most(a.requests, token, [&](int y) { return (int64_t)first_token(a, y); });
+            known = (int)token;
+            if (item == item0 + x) r = owner, i = known, h = (int)(item - token * a.Hq), mine = owner >= 0;
+        }
+        if (mine) {
+            new_tokens(a, r, first, n);
+            i -= first;
+            mine = i < min(n, a.max_new);
+        }
+    } else {                                           // request, new token, head
+        const int64_t per_request = (int64_t)a.max_new * a.Hq, request = item / per_request;
+        const int rest = (int)(item - request * per_request);
+        i = rest / a.Hq, h = rest - i * a.Hq;
+        if (request < a.requests) {
+            r = (int)request;
+            new_tokens(a, r, first, n);
+            mine = i < n;
+        }
+    }
+    const int g = h / a.G;
+    if (mine) {
+        const int len = suffix_len(a, r);
+        parts = a.prefix_splits;
+        if (len > 0) {
+            const int each = suffix_split_keys(len, a.suffix_splits);
+            parts += (len + each - 1) / each;
         }
     }
     const int64_t step = (int64_t)a.Hkv * a.rows, row = (int64_t)g * a.rows + (int64_t)(first + i) * a.G + (h - g * a.G);
@@ -710,7 +767,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         }
         m = top;
     }
-    if (i >= n) return;                                // (n is 0 behind the last request)
+    if (!mine) return;
     write_row<T>(a, first + i, h, lane, o, l, m);
 }
 
@@ -727,14 +784,13 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
             hipLaunchKernelGGL((small_attn_kernel<T, D, Small>), dim3((unsigned)(a.requests * a.Hkv)), dim3(64 * Small::kWaves), 0, stream, a);
             return check_launch();
         }
-    const int64_t own_groups = p.suffix_splits > 0 ? (int64_t)a.requests * a.Hkv * p.suffix_row_tiles * p.suffix_splits : 0;
     // several groups of lanes per row where there are parts for them
     constexpr int kGroups = 4 * kJoinThreads / D;
     const bool many = p.prefix_splits + p.suffix_splits > 4;
-    const int64_t joined = (int64_t)a.requests * a.max_new * a.Hq, joins = many ? joined : (joined + kGroups - 1) / kGroups;
-    if (a.prefix_groups + own_groups > 1 << 22 || joins > 1 << 23) return STEM_ERR_UNSUPPORTED;   // threads of a launch: 32 bits
-    const dim3 grid((unsigned)(a.prefix_groups + own_groups));
-    if (grid.x > 0) {
+    // (a line of a grid has less than 2^32 threads, and where there are lines each begins with a workgroup of XCD 0)
+    auto grid_of = [](int64_t n) { return n <= 1 << 20 ? dim3((unsigned)n) : dim3(1 << 20, (unsigned)((n + (1 << 20) - 1) >> 20)); };
+    const dim3 grid = grid_of(p.groups), joins = grid_of(many ? p.join_rows : (p.join_rows + kGroups - 1) / kGroups);
+    if (p.groups > 0) {
 #define STEM_PREFIX_LAUNCH(SP, SO) \
     hipLaunchKernelGGL((prefix_attn_kernel<T, D, SP, SO>), grid, dim3(64 * SP::kWaves), 0, stream, a)
         const bool few = p.suffix_row_tile == 16;
@@ -748,8 +804,8 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
 #undef STEM_PREFIX_LAUNCH
         if (const int st = check_launch()) return st;
     }
-    if (many) hipLaunchKernelGGL((join_kernel<T, D, kGroups>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
-    else hipLaunchKernelGGL((join_kernel<T, D, 1>), dim3((unsigned)joins), dim3(kJoinThreads), 0, stream, a);
+    if (many) hipLaunchKernelGGL((join_kernel<T, D, kGroups>), joins, dim3(kJoinThreads), 0, stream, a);
+    else hipLaunchKernelGGL((join_kernel<T, D, 1>), joins, dim3(kJoinThreads), 0, stream, a);
     return check_launch();
 }
 
@@ -774,9 +830,8 @@ int launch_prefix_attn(const PrefixCall& c, hipStream_t stream) {
     a.table_row = s.pages_per_request;
     a.page_shift = s.max_suffix > 0 ? __builtin_ctz(s.pages.page_size) : 0;
     a.num_pages = s.pages.num_pages;
-    const int64_t combos = ((int64_t)a.Hkv * p.prefix_splits + 7) / 8 * 8;
-    if (combos * p.row_tiles > 1 << 23) return STEM_ERR_UNSUPPORTED;
-    a.prefix_groups = (int32_t)(combos * p.row_tiles);
+    a.prefix_groups = (int32_t)p.prefix_groups, a.groups = (int32_t)p.groups;
+    a.own_by_rows = p.own_by_rows, a.join_by_rows = p.join_by_rows;
     a.q_st = s.q_stride_token, a.q_sh = s.q_stride_head, a.p_st = s.prefix_stride_token, a.p_sh = s.prefix_stride_head;
     a.page_st = s.pages.stride_page, a.tok_st = s.pages.stride_token, a.head_st = s.pages.stride_head;
     if (s.dtype == STEM_BF16) {

@@ -2,6 +2,7 @@
 host-only build, launchers replaced), and what it refuses."""
 import ctypes
 import os
+import random
 import shutil
 import subprocess
 
@@ -64,3 +65,47 @@ def test_longer_suffixes_are_refused():
     for suffix in (MOST_SUFFIX + 1, 2 ** 31 - 256, 2 ** 31 - 1):
         c = shape(requests=2, tokens=2, max_suffix=suffix, pages_per_request=1 << 27)
         assert db.lib().stem_prefix_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(n)) == NO
+
+
+def launches(host, c, units=256):
+    out = (ctypes.c_int64 * 6)()
+    status = host.stem_test_prefix_launches(ctypes.byref(c), units, out)
+    return status, dict(zip(("prefix_groups", "groups", "own_slots", "own_by_rows", "join_rows", "join_by_rows"), list(out)))
+
+
+@pytest.mark.parametrize("requests,tokens,max_new", [(300, 8192, 8192), (256, 512, 2048), (64, 64, 4097), (64, 2111, 2048), (1, 1, 1 << 25),
+                                                     (65536, 65536, 1 << 25)])
+def test_launches_go_by_the_rows_that_there_are(host, requests, tokens, max_new):
+    """However many new tokens a request is allowed: calls of few rows are not refused for it, and launch no more than they need."""
+    c = shape(requests=requests, tokens=tokens, max_new=max_new, pages_per_request=64)
+    status, l = launches(host, c)
+    assert status == sb.STEM_OK
+    assert l["join_rows"] <= tokens * 32
+    assert l["own_slots"] <= tokens * 4 // 16 + requests
+    p = plan(host, c)
+    assert l["groups"] - l["prefix_groups"] == l["own_slots"] * 8 * p["own_splits"]
+
+
+def test_calls_that_are_too_large_are_refused_with_their_workspace(host):
+    for kw in (dict(tokens=(2 ** 31 - 1) // 32, max_new=(2 ** 31 - 1) // 32), dict(requests=65536, num_q_heads=65535, num_kv_heads=65535, tokens=1000, max_new=1, head_dim=64,
+                                                      max_suffix=64, pages_per_request=4)):
+        status, _ = launches(host, shape(**kw))
+        assert status == NO, kw
+
+
+@pytest.mark.parametrize("G,tile", [(1, 16), (4, 64), (7, 64), (3, 16), (40, 64), (1, 64)])
+def test_every_row_tile_has_a_slot(host, G, tile):
+    """The slots of a request's row tiles are its own, as many as it has tiles, and within those that a call has."""
+    host.stem_test_slot_before.restype = ctypes.c_int64
+    host.stem_test_slot_before.argtypes = [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32]
+    r = random.Random(G * tile)
+    for _ in range(200):
+        new = [r.choice([0, 0, 1, 1, r.randint(0, 300)]) for _ in range(r.randint(1, 40))]
+        cu = [0]
+        for n in new:
+            cu.append(cu[-1] + n)
+        before = [host.stem_test_slot_before(x, y * G, tile) for x, y in enumerate(cu)]
+        for x, n in enumerate(new):
+            assert before[x + 1] - before[x] >= -(-n * G // tile) and before[x + 1] > before[x]
+        # and all of them within what a call of so many tokens, and any behind them, has
+        assert before[-1] <= host.stem_test_slot_before(len(new), (cu[-1] + r.randint(0, 9)) * G, tile)
