@@ -15,6 +15,7 @@
  *
  *   - dtype is STEM_BF16 or STEM_FP16 (stem_rotary and stem_rotary_append also take STEM_FP32); all of a call's tensors of
  *     values share it.
+ *   - With 0 tokens stem_rotary, stem_rotary_append and stem_prefix_attn do nothing, and their tensors' addresses are not looked at.
  *   - The last dimension is contiguous.  Strides are in elements and multiples of 8, base pointers of values 16-byte aligned,
  *     those of whole numbers aligned to their size.
  *   - Pages: k_pages and v_pages hold num_pages pages of page_size tokens of num_kv_heads rows of head_dim values, with

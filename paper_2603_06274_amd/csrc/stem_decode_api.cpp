@@ -32,8 +32,7 @@ static int check_pages(const stem_pages& p, int32_t head_dim) {
     return STEM_OK;
 }
 
-static int check_rotary(const stem_rotary_shape* s, const void* q, const void* k, const int32_t* positions,
-                        const double* turns, float factor, const void* q_out) {
+static int check_rotary(const stem_rotary_shape* s, float factor) {
     if (!s) return STEM_ERR_INVALID_ARG;
     if (s->dtype != STEM_BF16 && s->dtype != STEM_FP16 && s->dtype != STEM_FP32) return STEM_ERR_INVALID_ARG;
     if (s->tokens < 0 || s->num_q_heads < 0 || s->num_kv_heads < 0) return STEM_ERR_INVALID_ARG;
@@ -43,18 +42,24 @@ static int check_rotary(const stem_rotary_shape* s, const void* q, const void* k
     if (s->rotary_dim < 2 || s->rotary_dim % 2 || s->rotary_dim > s->head_dim) return STEM_ERR_INVALID_ARG;
     if (s->layout != STEM_ROTARY_HALF && s->layout != STEM_ROTARY_INTERLEAVED) return STEM_ERR_INVALID_ARG;
     if (!std::isfinite(factor)) return STEM_ERR_INVALID_ARG;
-    if (!positions || !aligned(positions, 4) || !turns || !aligned(turns, 8)) return STEM_ERR_INVALID_ARG;
     if (s->num_q_heads > 0) {
-        if (!q || !aligned(q, 16) || !q_out || !aligned(q_out, 16)) return STEM_ERR_INVALID_ARG;
         if (!good_strides(s->q_stride_token, s->q_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
         if (!good_strides(s->q_out_stride_token, s->q_out_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
-        if (q == q_out && (s->q_stride_token != s->q_out_stride_token || s->q_stride_head != s->q_out_stride_head))
+    }
+    if (s->num_kv_heads > 0 && !good_strides(s->k_stride_token, s->k_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
+    return STEM_OK;
+}
+
+// Of a call that has tokens (an empty tensor has no address).
+static int check_rotary_addresses(const stem_rotary_shape& s, const void* q, const void* k, const int32_t* positions,
+                                  const double* turns, const void* q_out) {
+    if (!positions || !aligned(positions, 4) || !turns || !aligned(turns, 8)) return STEM_ERR_INVALID_ARG;
+    if (s.num_q_heads > 0) {
+        if (!q || !aligned(q, 16) || !q_out || !aligned(q_out, 16)) return STEM_ERR_INVALID_ARG;
+        if (q == q_out && (s.q_stride_token != s.q_out_stride_token || s.q_stride_head != s.q_out_stride_head))
             return STEM_ERR_INVALID_ARG;
     }
-    if (s->num_kv_heads > 0) {
-        if (!k || !aligned(k, 16)) return STEM_ERR_INVALID_ARG;
-        if (!good_strides(s->k_stride_token, s->k_stride_head, s->head_dim)) return STEM_ERR_INVALID_ARG;
-    }
+    if (s.num_kv_heads > 0 && (!k || !aligned(k, 16))) return STEM_ERR_INVALID_ARG;
     return STEM_OK;
 }
 
@@ -228,16 +233,17 @@ int stem_rotary_frequencies(int32_t rotary_dim, double theta, const stem_rotary_
 int stem_rotary(const stem_rotary_shape* shape, const void* q, const void* k, const int32_t* positions,
                 const double* turns, float attention_factor, int32_t backward, void* q_out, void* k_out,
                 void* hip_stream) {
-    if (const int st = check_rotary(shape, q, k, positions, turns, attention_factor, q_out)) return st;
+    if (const int st = check_rotary(shape, attention_factor)) return st;
     if (backward != 0 && backward != 1) return STEM_ERR_INVALID_ARG;
     const stem_rotary_shape& s = *shape;
+    if (s.num_kv_heads > 0 && !good_strides(s.k_out_stride_token, s.k_out_stride_head, s.head_dim)) return STEM_ERR_INVALID_ARG;
+    if (s.tokens == 0) return STEM_OK;
+    if (const int st = check_rotary_addresses(s, q, k, positions, turns, q_out)) return st;
     if (s.num_kv_heads > 0) {
         if (!k_out || !aligned(k_out, 16)) return STEM_ERR_INVALID_ARG;
-        if (!good_strides(s.k_out_stride_token, s.k_out_stride_head, s.head_dim)) return STEM_ERR_INVALID_ARG;
         if (k == k_out && (s.k_stride_token != s.k_out_stride_token || s.k_stride_head != s.k_out_stride_head))
             return STEM_ERR_INVALID_ARG;
     }
-    if (s.tokens == 0) return STEM_OK;
     const RotaryCall call = {s, q, k, nullptr, q_out, k_out, nullptr, positions, nullptr, turns, attention_factor, backward, {}};
     return launch_rotary(call, static_cast<hipStream_t>(hip_stream));
 }
@@ -245,13 +251,15 @@ int stem_rotary(const stem_rotary_shape* shape, const void* q, const void* k, co
 int stem_rotary_append(const stem_rotary_shape* shape, const stem_pages* pages, const void* q, const void* k,
                        const void* v, const int32_t* positions, const int32_t* slots, const double* turns,
                        float attention_factor, void* q_out, void* k_pages, void* v_pages, void* hip_stream) {
-    if (const int st = check_rotary(shape, q, k, positions, turns, attention_factor, q_out)) return st;
+    if (const int st = check_rotary(shape, attention_factor)) return st;
     const stem_rotary_shape& s = *shape;
     if (!pages || s.num_kv_heads == 0) return STEM_ERR_INVALID_ARG;
     if (const int st = check_pages(*pages, s.head_dim)) return st;
+    if (s.tokens == 0) return STEM_OK;
+    if (const int st = check_rotary_addresses(s, q, k, positions, turns, q_out)) return st;
     if (!slots || !aligned(slots, 4) || !v || !aligned(v, 16)) return STEM_ERR_INVALID_ARG;
+    if (pages->num_pages == 0) return STEM_OK;
     if (!k_pages || !aligned(k_pages, 16) || !v_pages || !aligned(v_pages, 16)) return STEM_ERR_INVALID_ARG;
-    if (s.tokens == 0 || pages->num_pages == 0) return STEM_OK;
     const RotaryCall call = {s, q, k, v, q_out, k_pages, v_pages, positions, slots, turns, attention_factor, 0, *pages};
     return launch_rotary(call, static_cast<hipStream_t>(hip_stream));
 }
@@ -298,8 +306,10 @@ int stem_prefix_attn(const stem_prefix_shape* shape, const void* q, const void* 
                      size_t workspace_bytes, void* hip_stream) {
     if (const int st = check_prefix(shape)) return st;
     const stem_prefix_shape& s = *shape;
-    if (!q || !aligned(q, 16) || !out || !aligned(out, 16) || q == out || !aligned(lse, 4)) return STEM_ERR_INVALID_ARG;
     if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.f)) return STEM_ERR_INVALID_ARG;
+    if (!aligned(cu_new, 4) || (!cu_new && s.tokens != s.requests)) return STEM_ERR_INVALID_ARG;
+    if (s.tokens == 0) return STEM_OK;
+    if (!q || !aligned(q, 16) || !out || !aligned(out, 16) || q == out || !aligned(lse, 4)) return STEM_ERR_INVALID_ARG;
     if (s.prefix_len > 0 && (!prefix_k || !aligned(prefix_k, 16) || !prefix_v || !aligned(prefix_v, 16)))
         return STEM_ERR_INVALID_ARG;
     if (s.max_suffix > 0) {
@@ -307,9 +317,7 @@ int stem_prefix_attn(const stem_prefix_shape* shape, const void* q, const void* 
         if (s.pages.num_pages > 0 && (!k_pages || !aligned(k_pages, 16) || !v_pages || !aligned(v_pages, 16)))
             return STEM_ERR_INVALID_ARG;
     }
-    if (!aligned(cu_new, 4) || (!cu_new && s.tokens != s.requests)) return STEM_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 16)) return STEM_ERR_INVALID_ARG;
-    if (s.tokens == 0) return STEM_OK;
     PrefixCall call = {s, {}, q, prefix_k, prefix_v, k_pages, v_pages, table, lens, cu_new, softmax_scale, out, lse, workspace};
     if (const int st = prefix_plan(s, &call.plan)) return st;
     if (workspace_bytes < call.plan.bytes) return STEM_ERR_WORKSPACE;
