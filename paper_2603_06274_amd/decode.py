@@ -18,6 +18,8 @@ class Rotary:
                  high: float = 4.0, device="cuda"):
         self.head_dim, self.rotary_dim, self.layout = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), layout
         turns, self.attention_factor = db.stem_rotary_frequencies(self.rotary_dim, theta, scaling, factor, trained_length, low, high)
+        if self.rotary_dim > self.head_dim or self.head_dim % 8 or self.head_dim > db.STEM_MAX_HEAD_DIM or layout not in db.LAYOUTS:
+            raise ValueError("there are no positions of %d of %d values, layout %r" % (self.rotary_dim, self.head_dim, layout))
         self.turns = turns.to(device)
 
     @classmethod
@@ -58,6 +60,8 @@ class PagedCache:
     def __init__(self, requests: int, num_pages: int, page_size: int, pages_per_request: int, num_kv_heads: int, head_dim: int,
                  tokens: Optional[int] = None, position_offset: int = 0, dtype: torch.dtype = torch.bfloat16, device="cuda"):
         self.requests, self.tokens = int(requests), int(tokens if tokens is not None else requests)
+        if self.tokens > db.MAX_TOKENS:
+            raise ValueError("a step has at most %d rows" % db.MAX_TOKENS)
         self.k_pages, self.v_pages = (torch.empty(num_pages, page_size, num_kv_heads, head_dim, dtype=dtype, device=device)
                                       for _ in range(2))
         self.pages = db.PageShape.from_tensors(self.k_pages, self.v_pages)
@@ -95,8 +99,9 @@ class PagedCache:
             raise ValueError("k does not go with the cache's pages")
         if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
             raise ValueError("v has to be of k's sizes, strides and type")
-        if any(t is not None and t.device != self.k_pages.device for t in (q, k, v, q_out)):
+        if any(t is not None and t.device != self.k_pages.device for t in (q, k, v, q_out, rotary.turns)):
             raise ValueError("a step's tensors have to be on the cache's device")
+        db.need_usable_rows(shape, q, k, v, q_out)
         return shape
 
     def append(self, rotary: Rotary, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
@@ -131,6 +136,12 @@ class StemDecode:
         self.out = torch.zeros_like(self.q)
         self.lse = torch.zeros(num_q_heads, cache.tokens, dtype=torch.float32, device=dev) if want_lse else None
         self.shape = db.PrefixShape.from_tensors(self.q, prefix_k, cache.pages, cache.table, max_new, cache.max_suffix)
+        # all that the library could refuse of a step, but for its rows: a step that has begun is one that ends
+        db.need_usable_prefix(self.shape, prefix_k, prefix_v, self.softmax_scale)
+        if any(t.device != cache.k_pages.device for t in (prefix_k, prefix_v, self.rotary.turns)):
+            raise ValueError("the prefix and the positions have to be on the cache's device")
+        if num_q_heads + 2 * prefix_k.shape[1] > db.MAX_HEADS:
+            raise ValueError("a token has at most %d heads in all" % db.MAX_HEADS)
         self.workspace = torch.empty(db.stem_prefix_attn_workspace_bytes(self.shape), dtype=torch.uint8, device=dev)
 
     def attend(self) -> torch.Tensor:

@@ -8,6 +8,7 @@ Every step runs inside the library's HIP kernels on torch's current stream; ther
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Optional, Tuple
 
 import torch
@@ -22,6 +23,8 @@ DTYPES = {torch.bfloat16: STEM_BF16, torch.float16: STEM_FP16, torch.float32: ST
 LAYOUTS = {"half": STEM_ROTARY_HALF, "interleaved": STEM_ROTARY_INTERLEAVED}
 SCALINGS = {"none": STEM_ROTARY_NONE, "linear": STEM_ROTARY_LINEAR, "ntk": STEM_ROTARY_NTK, "yarn": STEM_ROTARY_YARN,
             "bands": STEM_ROTARY_BANDS}
+
+STEM_MAX_HEAD_DIM, MAX_TOKENS, MAX_HEADS = 1024, (1 << 24) - 1, 65535      # of stem_rotary and stem_rotary_append
 
 EXPORTED = ["stem_rotary_frequencies", "stem_rotary", "stem_block_table_workspace_bytes", "stem_block_table",
             "stem_rotary_append", "stem_prefix_attn_workspace_bytes", "stem_prefix_attn"]
@@ -198,6 +201,18 @@ def stem_rotary(shape: RotaryShape, q, k, positions: torch.Tensor, turns: torch.
                              stream), "stem_rotary")
 
 
+def need_usable_rows(shape: RotaryShape, *rows: Optional[torch.Tensor]) -> None:
+    """What the library asks of the rows of a call beyond their sizes: whole 16 bytes, and no row within another."""
+    c, at = shape.c, 0
+    strides = [c.k_stride_token, c.k_stride_head]
+    if c.num_q_heads > 0:
+        strides += (c.q_stride_token, c.q_stride_head, c.q_out_stride_token, c.q_out_stride_head)
+    for t in rows:
+        at |= 0 if t is None else t.data_ptr()
+    if at & 15 or min(strides) < c.head_dim or any(x & 7 for x in strides):
+        raise ValueError("rows have to begin at whole 16 bytes, %d or more elements apart" % c.head_dim)
+
+
 class PageShape:
     """Sizes and strides of k_pages and v_pages, both [num_pages, page_size, Hkv, d] with the same strides."""
 
@@ -293,6 +308,15 @@ class PrefixShape:
     @classmethod
     def from_tensors(cls, q, prefix_k, pages, table, max_new: int, max_suffix: int) -> "PrefixShape":
         return cls(q, prefix_k, pages, table, max_new, max_suffix)
+
+
+def need_usable_prefix(shape: PrefixShape, prefix_k, prefix_v, softmax_scale: float) -> None:
+    """What stem_prefix_attn asks of the prefix and of the scale."""
+    for t, name in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+        if shape.prefix is not None:
+            _need(_values(t, shape.prefix, name, prefix_k.get_device()) % 16 == 0, "%s has to begin at whole 16 bytes" % name)
+    scale = _f32(softmax_scale).value
+    _need(0.0 < scale < math.inf, "%r is no scale in fp32" % softmax_scale)
 
 
 def stem_prefix_attn_workspace_bytes(shape: PrefixShape) -> int:
