@@ -105,6 +105,7 @@ typedef struct stem_table_shape {
     int32_t pages_per_request;       /* entries of a table row, >= 1                                     */
     int32_t token_capacity;          /* entries of positions and slots, >= 0                             */
     int32_t position_offset;         /* position of a request's first own token (a shared prefix's length), >= 0 */
+    int32_t max_new;                 /* most new tokens of a request that the step's attention takes; 0: any number */
 } stem_table_shape;
 
 int stem_block_table_workspace_bytes(const stem_table_shape* shape, size_t* host_bytes);
@@ -122,8 +123,8 @@ int stem_block_table_workspace_bytes(const stem_table_shape* shape, size_t* host
  *     slot (-1 if the table's or ring's page is not one of the cache's).  From cu_new[requests] on (a padded batch)
  *     positions are 0 and slots -1.  ring_state_out is the ring's new state.
  *   - lens may be past_lens and ring_state_out may be ring_state; nothing else may overlap.
- *   - status int32 [4]: pages that are lacking; requests whose past length is negative or whose tokens a row cannot hold; tokens
- *     beyond token_capacity; pages given back that the ring has no room for (1 at least if ring_state is no state).  (Each
+ *   - status int32 [4]: pages that are lacking; requests whose past length is negative, whose tokens a row cannot hold or that have more
+ *     than max_new new ones; tokens beyond token_capacity; pages given back that the ring has no room for (1 at least if ring_state is no state).  (Each
  *     at most 2^31 - 1.)  Unless all are 0 the step is refused: table and ring are left as they are, lens and ring_state_out say what
  *     was, cu_new and positions are 0, slots -1.
  * workspace: 16-byte aligned, of stem_block_table_workspace_bytes, this call's alone until its work has finished.

@@ -74,7 +74,8 @@ TableWorkspace table_workspace(int32_t requests) {
 
 static int check_table(const stem_table_shape* s) {
     if (!s) return STEM_ERR_INVALID_ARG;
-    if (s->requests < 1 || s->num_pages < 1 || s->pages_per_request < 1 || s->token_capacity < 0 || s->position_offset < 0)
+    if (s->requests < 1 || s->num_pages < 1 || s->pages_per_request < 1 || s->token_capacity < 0 || s->position_offset < 0 ||
+        s->max_new < 0)
         return STEM_ERR_INVALID_ARG;
     if (const int st = check_page_size(s->page_size)) return st;
     if (s->requests > STEM_MAX_REQUESTS) return STEM_ERR_UNSUPPORTED;

@@ -18,6 +18,7 @@ struct TableArgs {
     int32_t *ring, *table, *lens, *ring_state_out, *cu_new, *positions, *slots, *status;
     int32_t *pages_before, *back_before, *ring_then;
     int32_t requests, num_pages, row, capacity, offset, shift;   // page_size = 1 << shift, row: entries of a table row
+    int32_t most_new;
 };
 
 // What a step does with one request.
@@ -30,7 +31,7 @@ __device__ __forceinline__ Step step_of(const TableArgs& a, int32_t past, int32_
     const int64_t most = (int64_t)a.row << a.shift;
     const bool gone = fresh < 0;
     s.more = gone ? 0 : fresh;
-    s.bad = past < 0 || (int64_t)past + s.more > most;
+    s.bad = past < 0 || (int64_t)past + s.more > most || s.more > a.most_new;
     if (s.bad) {                                       // counted, and then nothing is done at all
         s.past = s.have = s.need = s.back = s.more = 0;
         return s;
@@ -210,7 +211,8 @@ int launch_block_table(const TableCall& c, hipStream_t stream) {
     const stem_table_shape& s = c.shape;
     const TableArgs a = {c.past_lens, c.new_lens, c.ring_state, c.ring, c.table, c.lens, c.ring_state_out, c.cu_new, c.positions,
                          c.slots, c.status, c.pages_before, c.back_before, c.ring_then, s.requests, s.num_pages,
-                         s.pages_per_request, s.token_capacity, s.position_offset, __builtin_ctz(s.page_size)};
+                         s.pages_per_request, s.token_capacity, s.position_offset, __builtin_ctz(s.page_size),
+                         s.max_new > 0 ? s.max_new : 0x7fffffff};
     // One launch where a step is about a token per request, two where requests have many: a wave takes its long requests one after the
     // other.  One launch / two, us a call: 64 requests of one token 7.9 / 11.0, 1000 of one 10.4 / 11.4, 16 of 40 tokens on average 9.7 / 11.6, 64 of 29
     // 32.1 / 11.5, 256 of 7 28.5 / 11.4.  (And not where a finished request can have thousands of pages to give back.)

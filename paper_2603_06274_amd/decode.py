@@ -78,16 +78,17 @@ class PagedCache:
         self.ring_state = torch.tensor([0, num_pages], dtype=torch.int32, device=device)
         self.workspace = torch.empty(db.stem_block_table_workspace_bytes(self.shape), dtype=torch.uint8, device=device)
 
-    def advance(self, new_lens: Optional[torch.Tensor] = None) -> None:
+    def advance(self, new_lens: Optional[torch.Tensor] = None, max_new: int = 0) -> None:
         """Room for a step: new_lens int32 [requests] new tokens (None: one each; negative: the request has finished and its pages
-        go back).  Brings lens, table, cu_new, positions and slots up to date; a step for which there is no room changes none of
-        the first two, has no tokens and says so in status (see refused)."""
+        go back), each at most max_new (0: any number).  Brings lens, table, cu_new, positions and slots up to date; a step for which
+        there is no room changes none of the first two, has no tokens and says so in status (see refused)."""
+        self.shape.c.max_new = int(max_new)
         db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
                             self.cu_new, self.positions, self.slots, self.status, self.workspace)
 
     def refused(self) -> Tuple[int, int, int, int]:
-        """What the last step lacked: pages; requests with unusable lengths or too long for their row; tokens beyond the step's rows; room
-        for pages given back.  Waits for the GPU."""
+        """What the last step lacked: pages; requests with unusable lengths, too long for their row or of more new tokens than allowed;
+        tokens beyond the step's rows; room for pages given back.  Waits for the GPU."""
         return tuple(self.status.tolist())
 
     def _rows_shape(self, rotary: Rotary, q, k, v, q_out) -> db.RotaryShape:
@@ -132,6 +133,7 @@ class StemDecode:
         if self.rotary.head_dim != d:
             raise ValueError("heads of %d values, and positions made for %d" % (d, self.rotary.head_dim))
         self.softmax_scale = float(softmax_scale if softmax_scale is not None else d ** -0.5)
+        self.max_new = int(max_new)
         self.q = torch.zeros(cache.tokens, num_q_heads, d, dtype=dtype, device=dev)      # turned
         self.out = torch.zeros_like(self.q)
         self.lse = torch.zeros(num_q_heads, cache.tokens, dtype=torch.float32, device=dev) if want_lse else None
@@ -152,9 +154,10 @@ class StemDecode:
         return self.out
 
     def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, new_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """One step: room for the new tokens, their keys and values into the cache, their attention.  Rows as in PagedCache.append; at most
-        max_new tokens per request.  Returns self.out, whose rows behind the last new token keep what they held."""
+        """One step: room for the new tokens, their keys and values into the cache, their attention.  Rows as in PagedCache.append; a
+        step with more than max_new tokens of a request is one without room.  Returns self.out, whose rows behind the last new token
+        keep what they held."""
         shape = self.cache._rows_shape(self.rotary, q, k, v, self.q)      # (what it refuses leaves the cache as it was)
-        self.cache.advance(new_lens)
+        self.cache.advance(new_lens, self.max_new)
         self.cache._write(shape, self.rotary, q, k, v, self.q)
         return self.attend()

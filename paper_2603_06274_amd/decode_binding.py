@@ -45,7 +45,7 @@ class stem_rotary_shape(ctypes.Structure):
 
 class stem_table_shape(ctypes.Structure):
     _fields_ = [(x, _i32) for x in ("requests", "page_size", "num_pages", "pages_per_request", "token_capacity",
-                                    "position_offset")]
+                                    "position_offset", "max_new")]
 
 
 class stem_pages(ctypes.Structure):
@@ -247,12 +247,12 @@ def stem_rotary_append(shape: RotaryShape, pages: PageShape, q, k, v, positions:
 
 
 class TableShape:
-    """Sizes of a block table and of the step that it is brought up to date for."""
+    """Sizes of a block table and of the step that it is brought up to date for; max_new 0: any number of new tokens per request."""
 
     def __init__(self, requests: int, page_size: int, num_pages: int, pages_per_request: int, token_capacity: int,
-                 position_offset: int = 0):
+                 position_offset: int = 0, max_new: int = 0):
         self.c = stem_table_shape(int(requests), int(page_size), int(num_pages), int(pages_per_request), int(token_capacity),
-                                  int(position_offset))
+                                  int(position_offset), int(max_new))
         self.ref = ctypes.byref(self.c)
 
 
