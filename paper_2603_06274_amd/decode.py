@@ -55,17 +55,20 @@ class Rotary:
 class PagedCache:
     """Keys and values of up to `requests` requests in `num_pages` pages of `page_size` tokens, at most `pages_per_request` each, with the
     block tables, lengths and free pages that go with them, all on the GPU.  `tokens` is the number of rows of a step's tensors: a step has
-    at most that many new tokens.  `position_offset`: the position of a request's first token (a shared prefix's length)."""
+    at most that many new tokens.  `position_offset`: the position of a request's first token.  Where it is not given, the first
+    StemDecode with rotary positions that is made of the cache sets it to the length of its prefix; a cache that begins before that begins at 0."""
 
     def __init__(self, requests: int, num_pages: int, page_size: int, pages_per_request: int, num_kv_heads: int, head_dim: int,
-                 tokens: Optional[int] = None, position_offset: int = 0, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+                 tokens: Optional[int] = None, position_offset: Optional[int] = None, dtype: torch.dtype = torch.bfloat16, device="cuda"):
         self.requests, self.tokens = int(requests), int(tokens if tokens is not None else requests)
         if self.tokens > db.MAX_TOKENS:
             raise ValueError("a step has at most %d rows" % db.MAX_TOKENS)
         self.k_pages, self.v_pages = (torch.empty(num_pages, page_size, num_kv_heads, head_dim, dtype=dtype, device=device)
                                       for _ in range(2))
         self.pages = db.PageShape.from_tensors(self.k_pages, self.v_pages)
-        self.shape = db.TableShape(requests, page_size, num_pages, pages_per_request, self.tokens, position_offset)
+        self.shape = db.TableShape(requests, page_size, num_pages, pages_per_request, self.tokens, position_offset or 0)
+        self._offset_open = position_offset is None        # whether the first position may still be set
+        self.offset_given = position_offset is not None
         self.max_suffix = int(pages_per_request) * int(page_size)
 
         def whole(*sizes, value=0):
@@ -83,8 +86,22 @@ class PagedCache:
         go back), each at most max_new (0: any number).  Brings lens, table, cu_new, positions and slots up to date; a step for which
         there is no room changes none of the first two, has no tokens and says so in status (see refused)."""
         self.shape.c.max_new = int(max_new)
+        self._offset_open = False
         db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
                             self.cu_new, self.positions, self.slots, self.status, self.workspace)
+
+    def begin_behind(self, length: int) -> None:
+        """The requests' first position is `length`, unless another was given when the cache was made.  Raises if the cache has begun, or
+        has been set to begin, elsewhere."""
+        offset = self.shape.c.position_offset
+        if self.offset_given or offset == length:
+            return
+        if not self._offset_open or offset:
+            raise ValueError("the cache's positions begin at %d, behind a prefix of %d tokens" % (offset, length))
+        # (the sizes as they would be from the start, which the library may refuse)
+        c = self.shape.c
+        db.stem_block_table_workspace_bytes(db.TableShape(c.requests, c.page_size, c.num_pages, c.pages_per_request, c.token_capacity, length))
+        c.position_offset = length
 
     def refused(self) -> Tuple[int, int, int, int]:
         """What the last step lacked: pages; requests with unusable lengths, too long for their row or of more new tokens than allowed;
@@ -121,7 +138,8 @@ class PagedCache:
 
 class StemDecode:
     """Decoding steps of the requests of a PagedCache behind a prefix that they share: prefix_k, prefix_v [L, Hkv, d], its keys turned
-    already, as StemPrefill leaves them.  One object is one sequence of steps: its buffers belong to one step at a time.  A step may be
+    already, as StemPrefill leaves them.  With rotary positions, new tokens stand behind the prefix, at L and on, unless the cache was
+    made with a position_offset (for keys whose positions do not begin at 0).  One object is one sequence of steps: its buffers belong to one step at a time.  A step may be
     captured into a graph and replayed."""
 
     def __init__(self, prefix_k: torch.Tensor, prefix_v: torch.Tensor, num_q_heads: int, cache: PagedCache,
@@ -145,6 +163,8 @@ class StemDecode:
         if num_q_heads + 2 * prefix_k.shape[1] > db.MAX_HEADS:
             raise ValueError("a token has at most %d heads in all" % db.MAX_HEADS)
         self.workspace = torch.empty(db.stem_prefix_attn_workspace_bytes(self.shape), dtype=torch.uint8, device=dev)
+        if rotary is not None:
+            cache.begin_behind(prefix_k.shape[0])
 
     def attend(self) -> torch.Tensor:
         """Attention of self.q's rows, whose keys and values are in the cache, to the prefix and to their requests' tokens."""

@@ -114,11 +114,11 @@ class StemPrefill:
 
     def decode(self, cache: PagedCache, sequence: int = 0, max_new: int = 1, want_lse: bool = False) -> StemDecode:
         """Decoding steps of the cache's requests behind one of the pre-filled sequences, with this layer's rotary positions and scale.
-        With rotary positions, the cache's position_offset has to be the sequence's length."""
+        With rotary positions, the cache's position_offset has to be the sequence's length (or not given)."""
         if not 0 <= sequence < len(self.shape.cu_seqlens) - 1:
             raise ValueError("there is no sequence %d" % sequence)
         rows = slice(self.shape.cu_seqlens[sequence], self.shape.cu_seqlens[sequence + 1])
-        if self.rotary is not None and cache.shape.c.position_offset != rows.stop - rows.start:
+        if self.rotary is not None and cache.offset_given and cache.shape.c.position_offset != rows.stop - rows.start:
             raise ValueError("the cache's positions begin at %d, behind a sequence of %d tokens" %
                              (cache.shape.c.position_offset, rows.stop - rows.start))
         return StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, self.rotary, max_new, self.softmax_scale, want_lse)
