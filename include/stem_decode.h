@@ -50,7 +50,7 @@ extern "C" {
  *           dim(n) = rotary_dim ln(trained_length / (2 pi n)) / (2 ln theta) is the pair that turns n times within the trained
  *           length, lo = max(floor(dim(high)), 0) and hi = min(ceil(dim(low)), rotary_dim - 1)   (arXiv 2309.00071)
  *   BANDS   f(i) y + f(i) / factor (1 - y), y = clamp((trained_length f(i) / (2 pi) - low) / (high - low), 0, 1)
- * low < high are numbers of turns within the trained length. */
+ * low < high are numbers of turns within the trained length (1 and 32 with YARN, 1 and 4 with BANDS, where a model says nothing else). */
 #define STEM_ROTARY_NONE    0
 #define STEM_ROTARY_LINEAR  1
 #define STEM_ROTARY_NTK     2

@@ -11,11 +11,11 @@ from . import decode_binding as db
 
 class Rotary:
     """Rotary positions of heads of `head_dim` values, of which the first `rotary_dim` turn (None: all), in the "half" or
-    "interleaved" layout, with frequencies scaled for long contexts by one of decode_binding.SCALINGS."""
+    "interleaved" layout, with frequencies scaled for long contexts by one of decode_binding.SCALINGS (low, high: as stem_rotary_frequencies has them)."""
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, theta: float = 10000.0, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, trained_length: float = 0.0, low: float = 1.0,
-                 high: float = 4.0, device="cuda"):
+                 high: Optional[float] = None, device="cuda"):
         self.head_dim, self.rotary_dim, self.layout = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), layout
         turns, self.attention_factor = db.stem_rotary_frequencies(self.rotary_dim, theta, scaling, factor, trained_length, low, high)
         if self.rotary_dim > self.head_dim or self.head_dim % 8 or self.head_dim > db.STEM_MAX_HEAD_DIM or layout not in db.LAYOUTS:

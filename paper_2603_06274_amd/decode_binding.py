@@ -145,9 +145,13 @@ def _seen(t: Optional[torch.Tensor]) -> Optional[tuple]:
 
 
 def stem_rotary_frequencies(rotary_dim: int, theta: float, scaling: str = "none", factor: float = 1.0,
-                            trained_length: float = 0.0, low: float = 1.0, high: float = 4.0) -> Tuple[torch.Tensor, float]:
-    """(turns float64 CPU tensor [rotary_dim / 2], attention factor) of a scaling method ("none", "linear", "ntk", "yarn", "bands")."""
+                            trained_length: float = 0.0, low: float = 1.0, high: Optional[float] = None) -> Tuple[torch.Tensor, float]:
+    """(turns float64 CPU tensor [rotary_dim / 2], attention factor) of a scaling method ("none", "linear", "ntk", "yarn", "bands").
+    low and high: numbers of turns within the trained length between which the scaling sets in; high None: the method's own, 32 for
+    "yarn" and 4 for "bands"."""
     _need(scaling in SCALINGS, "unknown scaling %r" % (scaling,))
+    if high is None:
+        high = 32.0 if scaling == "yarn" else 4.0
     c = stem_rotary_scaling(SCALINGS[scaling], float(factor), float(trained_length), float(low), float(high))
     out = torch.zeros(max(int(rotary_dim) // 2, 1), dtype=torch.float64)
     af = _f64()
