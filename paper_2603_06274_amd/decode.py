@@ -52,6 +52,17 @@ class Rotary:
         return self._run(grad_q, grad_k, positions, grad_q_out, grad_k_out, True)
 
 
+class Turned:
+    """Whether the buffers for a prompt's turned queries and keys hold them."""
+
+    def __init__(self, done: bool):
+        self.done = done
+
+    def need(self) -> None:
+        if not self.done:
+            raise RuntimeError("queries and keys have not been turned by their positions: run() or rotate() first")
+
+
 class PagedCache:
     """Keys and values of up to `requests` requests in `num_pages` pages of `page_size` tokens, at most `pages_per_request` each, with the
     block tables, lengths and free pages that go with them, all on the GPU.  `tokens` is the number of rows of a step's tensors: a step has
@@ -147,6 +158,7 @@ class StemDecode:
                  want_lse: bool = False):
         d, dev, dtype = prefix_k.shape[2], prefix_k.device, prefix_k.dtype
         self.prefix_k, self.prefix_v, self.cache = prefix_k, prefix_v, cache
+        self.turned = Turned(True)
         self.rotary = rotary if rotary is not None else Rotary.none(d, dev)
         if self.rotary.head_dim != d:
             raise ValueError("heads of %d values, and positions made for %d" % (d, self.rotary.head_dim))
@@ -168,6 +180,7 @@ class StemDecode:
 
     def attend(self) -> torch.Tensor:
         """Attention of self.q's rows, whose keys and values are in the cache, to the prefix and to their requests' tokens."""
+        self.turned.need()
         c = self.cache
         db.stem_prefix_attn(self.shape, self.q, self.prefix_k, self.prefix_v, c.k_pages, c.v_pages, c.table, c.lens, c.cu_new,
                             self.softmax_scale, self.out, self.lse, self.workspace)
@@ -177,6 +190,7 @@ class StemDecode:
         """One step: room for the new tokens, their keys and values into the cache, their attention.  Rows as in PagedCache.append; a
         step with more than max_new tokens of a request is one without room.  Returns self.out, whose rows behind the last new token
         keep what they held."""
+        self.turned.need()
         shape = self.cache._rows_shape(self.rotary, q, k, v, self.q)      # (what it refuses leaves the cache as it was)
         self.cache.advance(new_lens, self.max_new)
         self.cache._write(shape, self.rotary, q, k, v, self.q)

@@ -7,7 +7,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import binding as sb
-from .decode import PagedCache, Rotary, StemDecode
+from .decode import PagedCache, Rotary, StemDecode, Turned
 
 
 class StemPrefill:
@@ -17,7 +17,8 @@ class StemPrefill:
     chunk = (starts, ends), q holds only the tokens of each sequence's chunk (T = their sum) while
     k and v keep all Tk = cu_seqlens[-1] rows; pass the same `workspace` to the calls of one
     prompt so that the pooled keys of earlier chunks are kept.  With `rotary`, q and k are not yet turned: run() turns them by
-    their positions in their sequences into buffers of its own (self.q, self.k), which the stages use.
+    their positions in their sequences into buffers of its own (self.q, self.k), which the stages use.  A stage called by itself, or a
+    step of decode(), before run() or rotate() raises.
     """
 
     def __init__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: Sequence[int],
@@ -31,6 +32,7 @@ class StemPrefill:
         assert q.dtype == k.dtype == v.dtype == torch.bfloat16
         assert k.stride() == v.stride() and k.shape == v.shape
         self.rotary = rotary
+        self.turned = Turned(rotary is None)
         if rotary is not None:
             if chunk is not None:
                 raise ValueError("a chunk's queries and keys are turned before the call, with Rotary.apply")
@@ -72,13 +74,18 @@ class StemPrefill:
         self.lse = torch.empty((Hq, T), dtype=torch.float32, device=dev) if want_lse else None
 
     def rotate(self) -> None:
+        """q and k as they are now, turned into self.q and self.k.  Part of run(); before stages that are called one by one, it has to
+        be called whenever q or k have changed."""
         self.rotary.apply(*self.unturned, self.positions, self.q, self.k)
+        self.turned.done = True
 
     def estimate(self) -> None:
+        self.turned.need()
         sb.stem_estimate(self.shape, self.q, self.k, self.v, self.beta, self.route_scale,
                          self.ad_stride, self.scores, self.workspace, self.fill_scores)
 
     def pool(self) -> None:
+        self.turned.need()
         sb.stem_pool(self.shape, self.q, self.k, self.v, self.ad_stride, self.workspace)
 
     def block_scores(self) -> None:
@@ -95,6 +102,7 @@ class StemPrefill:
                        lists_per_kv_head=bool(self.group_share))
 
     def attend(self) -> None:
+        self.turned.need()
         if not self.queue_bytes:
             sb.stem_sparse_attn(self.shape, self.q, self.k, self.v, self.counts, self.indices, self.kmax,
                                 self.softmax_scale, self.out, self.lse, lists_per_kv_head=bool(self.group_share))
@@ -108,6 +116,7 @@ class StemPrefill:
     def estimate_select(self, debug_scores: Optional[torch.Tensor] = None) -> None:
         """Stages 1-2 without the score tensor (per-head lists only)."""
         assert not self.group_share
+        self.turned.need()
         sb.stem_estimate_select(self.shape, self.q, self.k, self.v, self.beta, self.route_scale,
                                 self.ad_stride, self.budget, self.n_sink, self.n_local, self.counts,
                                 self.indices, self.kmax, debug_scores, self.workspace)
@@ -121,7 +130,9 @@ class StemPrefill:
         if self.rotary is not None and cache.offset_given and cache.shape.c.position_offset != rows.stop - rows.start:
             raise ValueError("the cache's positions begin at %d, behind a sequence of %d tokens" %
                              (cache.shape.c.position_offset, rows.stop - rows.start))
-        return StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, self.rotary, max_new, self.softmax_scale, want_lse)
+        decode = StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, self.rotary, max_new, self.softmax_scale, want_lse)
+        decode.turned = self.turned
+        return decode
 
     def run(self, fused: bool = False) -> torch.Tensor:
         if self.rotary is not None:
