@@ -36,9 +36,9 @@ class StemPrefill:
         if rotary is not None:
             if chunk is not None:
                 raise ValueError("a chunk's queries and keys are turned before the call, with Rotary.apply")
-            self.unturned = q, k
-            self.positions = torch.cat([torch.arange(int(hi) - int(lo), dtype=torch.int32)
-                                        for lo, hi in zip(cu_seqlens, cu_seqlens[1:])]).to(q.device)
+            if min(q.shape[0], k.shape[0]) < int(cu_seqlens[-1]):
+                raise ValueError("q and k have fewer rows than the sequences")
+            self.unturned = tuple(x[:int(cu_seqlens[-1])] for x in (q, k))      # (rows behind the last sequence are nobody's)
             q, k = (torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) for x in (q, k))
         self.q, self.k, self.v = q, k, v
         self.shape = sb.Shape.from_tensors(q, k, block_size, cu_seqlens, chunk)
@@ -53,6 +53,9 @@ class StemPrefill:
         self.group_share = group_share
         self.softmax_scale = float(softmax_scale if softmax_scale is not None else q.shape[2] ** -0.5)
         self.rows, self.nbmax = sb.stem_rows(self.shape)
+        if rotary is not None:
+            self.positions = torch.cat([torch.arange(hi - lo, dtype=torch.int32)
+                                        for lo, hi in zip(self.shape.cu_seqlens, self.shape.cu_seqlens[1:])]).to(q.device)
         budget_host, kmax = sb.stem_budget_schedule(self.shape, k_start_blocks, mu, k_min, n_sink, n_local)
         self.budget_host = budget_host
         self.kmax = max(kmax, 1)
@@ -76,7 +79,8 @@ class StemPrefill:
     def rotate(self) -> None:
         """q and k as they are now, turned into self.q and self.k.  Part of run(); before stages that are called one by one, it has to
         be called whenever q or k have changed."""
-        self.rotary.apply(*self.unturned, self.positions, self.q, self.k)
+        n = self.shape.cu_seqlens[-1]
+        self.rotary.apply(*self.unturned, self.positions, self.q[:n], self.k[:n])
         self.turned.done = True
 
     def estimate(self) -> None:
