@@ -125,16 +125,21 @@ class StemPrefill:
                                 self.ad_stride, self.budget, self.n_sink, self.n_local, self.counts,
                                 self.indices, self.kmax, debug_scores, self.workspace)
 
-    def decode(self, cache: PagedCache, sequence: int = 0, max_new: int = 1, want_lse: bool = False) -> StemDecode:
+    def decode(self, cache: PagedCache, sequence: int = 0, max_new: int = 1, want_lse: bool = False,
+               rotary: Optional[Rotary] = None) -> StemDecode:
         """Decoding steps of the cache's requests behind one of the pre-filled sequences, with this layer's rotary positions and scale.
-        With rotary positions, the cache's position_offset has to be the sequence's length (or not given)."""
+        `rotary`: the positions of queries and keys that were turned before the call (a chunked prompt's, for one); without any, new
+        rows are taken as they come.  With rotary positions, the cache's position_offset has to be the sequence's length (or not given)."""
+        if rotary is not None and self.rotary is not None and rotary is not self.rotary:
+            raise ValueError("the keys were turned by other positions")
+        rotary = rotary if rotary is not None else self.rotary
         if not 0 <= sequence < len(self.shape.cu_seqlens) - 1:
             raise ValueError("there is no sequence %d" % sequence)
         rows = slice(self.shape.cu_seqlens[sequence], self.shape.cu_seqlens[sequence + 1])
-        if self.rotary is not None and cache.offset_given and cache.shape.c.position_offset != rows.stop - rows.start:
+        if rotary is not None and cache.offset_given and cache.shape.c.position_offset != rows.stop - rows.start:
             raise ValueError("the cache's positions begin at %d, behind a sequence of %d tokens" %
                              (cache.shape.c.position_offset, rows.stop - rows.start))
-        decode = StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, self.rotary, max_new, self.softmax_scale, want_lse)
+        decode = StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, rotary, max_new, self.softmax_scale, want_lse)
         decode.turned = self.turned
         return decode
 
