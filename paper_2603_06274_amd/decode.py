@@ -9,6 +9,27 @@ import torch
 from . import decode_binding as db
 
 
+class _Turn(torch.autograd.Function):
+    """Rotary._run as a node of autograd's graph: the gradients of either map are the other map of the gradients."""
+
+    @staticmethod
+    def forward(ctx, rotary, positions, q, k, backward):
+        ctx.rotary, ctx.is_backward = rotary, backward
+        ctx.save_for_backward(positions)
+        ctx.set_materialize_grads(False)
+        out = rotary._run(q, k, positions, None, None, backward)
+        ctx.mark_non_differentiable(*(y for y, needed in zip(out, ctx.needs_input_grad[2:4]) if y is not None and not needed))
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_q, grad_k):
+        # gradients come with any strides (one number for all rows, for instance): what the library does not take is copied
+        grads = [g if g is None or db.usable_rows(g) else g.clone(memory_format=torch.contiguous_format) for g in (grad_q, grad_k)]
+        if grads[0] is None and grads[1] is None:
+            return None, None, None, None, None
+        return (None, None, *_Turn.apply(ctx.rotary, *ctx.saved_tensors, *grads, not ctx.is_backward), None)
+
+
 class Rotary:
     """Rotary positions of heads of `head_dim` values, of which the first `rotary_dim` turn (None: all), in the "half" or
     "interleaved" layout, with frequencies scaled for long contexts by one of decode_binding.SCALINGS (low, high: as stem_rotary_frequencies has them)."""
@@ -35,6 +56,13 @@ class Rotary:
             raise ValueError("heads of %d values, and positions made for %d" % (shape.c.head_dim, self.head_dim))
         return shape
 
+    def _turn(self, q, k, positions, q_out, k_out, backward: bool) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+        if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, k)):
+            if q_out is not None or k_out is not None:
+                raise ValueError("outputs that are given carry no gradients: call under torch.no_grad, or without them")
+            return _Turn.apply(self, positions, q, k, backward)
+        return self._run(q, k, positions, q_out, k_out, backward)
+
     def _run(self, q, k, positions, q_out, k_out, backward: bool) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
         q_out = torch.empty_like(q) if q_out is None and q is not None else q_out
         k_out = torch.empty_like(k) if k_out is None and k is not None else k_out
@@ -44,12 +72,12 @@ class Rotary:
 
     def apply(self, q, k, positions: torch.Tensor, q_out=None, k_out=None):
         """q [T, Hq, d] and k [T, Hkv, d] (either may be None) turned by positions int32 [T]; into new tensors unless q_out and
-        k_out are given, which may be q and k themselves."""
-        return self._run(q, k, positions, q_out, k_out, False)
+        k_out are given, which may be q and k themselves.  New tensors carry q's and k's gradients."""
+        return self._turn(q, k, positions, q_out, k_out, False)
 
     def backward(self, grad_q, grad_k, positions: torch.Tensor, grad_q_out=None, grad_k_out=None):
         """The gradients of apply's inputs from those of its outputs."""
-        return self._run(grad_q, grad_k, positions, grad_q_out, grad_k_out, True)
+        return self._turn(grad_q, grad_k, positions, grad_q_out, grad_k_out, True)
 
 
 class Turned:

@@ -205,6 +205,12 @@ def stem_rotary(shape: RotaryShape, q, k, positions: torch.Tensor, turns: torch.
                              stream), "stem_rotary")
 
 
+def usable_rows(t: torch.Tensor) -> bool:
+    """Whether the library takes the strides and the address of rows [tokens, heads, head_dim]."""
+    _, _, d, token, head = _rows(t, "rows") if t.stride(-1) == 1 else (0, 0, 1, 0, 0)
+    return min(token, head) >= d and not (token | head) & 7 and not t.data_ptr() & 15
+
+
 def need_usable_rows(shape: RotaryShape, *rows: Optional[torch.Tensor]) -> None:
     """What the library asks of the rows of a call beyond their sizes: whole 16 bytes, and no row within another."""
     c, at = shape.c, 0

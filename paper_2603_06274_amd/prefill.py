@@ -80,7 +80,8 @@ class StemPrefill:
         """q and k as they are now, turned into self.q and self.k.  Part of run(); before stages that are called one by one, it has to
         be called whenever q or k have changed."""
         n = self.shape.cu_seqlens[-1]
-        self.rotary.apply(*self.unturned, self.positions, self.q[:n], self.k[:n])
+        with torch.no_grad():                              # (none of the stages carries gradients)
+            self.rotary.apply(*self.unturned, self.positions, self.q[:n], self.k[:n])
         self.turned.done = True
 
     def estimate(self) -> None:
