@@ -140,6 +140,14 @@ def _whole(t: Optional[torch.Tensor], n: int, name: str, dev: int, dtype: torch.
     return t.data_ptr()
 
 
+def _lines(t: Optional[torch.Tensor], n: int, each: int, name: str, dev: int, dtype: torch.dtype = torch.int32) -> int:
+    """Address of a contiguous tensor of n lines (or more) of `each` numbers; one of another number of dimensions than two is
+    taken for these lines one after the other."""
+    if t is not None and t.dim() == 2 and t.shape[1] != each:
+        raise ValueError("%s has lines of %d, not of %d" % (name, t.shape[1], each))
+    return _whole(t, n * each, name, dev, dtype)
+
+
 def _seen(t: Optional[torch.Tensor]) -> Optional[tuple]:
     return None if t is None else (t.shape, t.stride(), t.dtype)
 
@@ -281,7 +289,7 @@ def stem_block_table(shape: TableShape, past_lens: torch.Tensor, new_lens: Optio
     _check(lib().stem_block_table(
         shape.ref, _whole(past_lens, R, "past_lens", dev), None if new_lens is None else _whole(new_lens, R, "new_lens", dev),
         _whole(ring_state, 2, "ring_state", dev), _whole(ring, c.num_pages, "ring", dev),
-        _whole(table, R * c.pages_per_request, "table", dev), _whole(lens, R, "lens", dev),
+        _lines(table, R, c.pages_per_request, "table", dev), _whole(lens, R, "lens", dev),
         _whole(ring_state_out, 2, "ring_state_out", dev), _whole(cu_new, R + 1, "cu_new", dev),
         _whole(positions, c.token_capacity, "positions", dev), _whole(slots, c.token_capacity, "slots", dev),
         _whole(status, 4, "status", dev), _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(),
@@ -344,8 +352,8 @@ def stem_prefix_attn(shape: PrefixShape, q: torch.Tensor, prefix_k, prefix_v, k_
         shape.ref, _values(q, shape.q, "q", dev), _values(prefix_k, shape.prefix, "prefix_k", dev),
         _values(prefix_v, shape.prefix, "prefix_v", dev), _values(k_pages, shape.pages, "k_pages", dev) if paged else None,
         _values(v_pages, shape.pages, "v_pages", dev) if paged else None,
-        _whole(table, c.requests * c.pages_per_request, "table", dev) if paged else None,
+        _lines(table, c.requests, c.pages_per_request, "table", dev) if paged else None,
         _whole(lens, c.requests, "lens", dev) if paged else None,
         None if cu_new is None else _whole(cu_new, c.requests + 1, "cu_new", dev), softmax_scale,
-        _values(out, shape.q, "out", dev), None if lse is None else _whole(lse, c.num_q_heads * c.tokens, "lse", dev, torch.float32),
+        _values(out, shape.q, "out", dev), None if lse is None else _lines(lse, c.num_q_heads, c.tokens, "lse", dev, torch.float32),
         _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(), stream), "stem_prefix_attn")
