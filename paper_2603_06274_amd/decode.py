@@ -124,7 +124,7 @@ class PagedCache:
         """Room for a step: new_lens int32 [requests] new tokens (None: one each; negative: the request has finished and its pages
         go back), each at most max_new (0: any number).  Brings lens, table, cu_new, positions and slots up to date; a step for which
         there is no room changes none of the first two, has no tokens and says so in status (see refused)."""
-        self.shape.c.max_new = int(max_new)
+        self.shape.c.max_new = max_new
         self._offset_open = False
         db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
                             self.cu_new, self.positions, self.slots, self.status, self.workspace)
@@ -156,7 +156,8 @@ class PagedCache:
             raise ValueError("k does not go with the cache's pages")
         if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
             raise ValueError("v has to be of k's sizes, strides and type")
-        if any(t is not None and t.device != self.k_pages.device for t in (q, k, v, q_out, rotary.turns)):
+        dev = self.k_pages.device
+        if not k.device == v.device == rotary.turns.device == dev or q is not None and not q.device == q_out.device == dev:
             raise ValueError("a step's tensors have to be on the cache's device")
         db.need_usable_rows(shape, q, k, v, q_out)
         return shape

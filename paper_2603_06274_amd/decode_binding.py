@@ -143,9 +143,11 @@ def _whole(t: Optional[torch.Tensor], n: int, name: str, dev: int, dtype: torch.
 def _lines(t: Optional[torch.Tensor], n: int, each: int, name: str, dev: int, dtype: torch.dtype = torch.int32) -> int:
     """Address of a contiguous tensor of n lines (or more) of `each` numbers; one of another number of dimensions than two is
     taken for these lines one after the other."""
-    if t is not None and t.dim() == 2 and t.shape[1] != each:
-        raise ValueError("%s has lines of %d, not of %d" % (name, t.shape[1], each))
-    return _whole(t, n * each, name, dev, dtype)
+    if t is None or t.dtype is not dtype or t.numel() < n * each or not t.is_contiguous() or t.dim() == 2 and t.size(1) != each:
+        raise ValueError("%s has to be contiguous %s of at least %d lines of %d" % (name, dtype, n, each))
+    if t.get_device() != dev:
+        raise ValueError("%s is not on the current device" % name)
+    return t.data_ptr()
 
 
 def _seen(t: Optional[torch.Tensor]) -> Optional[tuple]:
@@ -177,25 +179,29 @@ class RotaryShape:
                  q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         _need(q is not None or k is not None, "q or k is needed")
         _need(layout in LAYOUTS, "unknown layout %r" % (layout,))
-        first = q if q is not None else k
-        self.c = c = stem_rotary_shape(_dtype(first, "q" if q is not None else "k"), first.shape[0], 0, 0, first.shape[-1],
-                                       int(rotary_dim), LAYOUTS[layout])
-        for x, given in (("q", q), ("k", k), ("q_out", q_out if q_out is not None else q),
-                         ("k_out", k_out if k_out is not None else k)):
-            if given is None:
-                continue
-            T, H, d, st, sh = _rows(given, x)
-            _need(given.dtype == first.dtype and T == c.tokens and d == c.head_dim, "%s does not go with the others" % x)
-            setattr(c, x + "_stride_token", st)
-            setattr(c, x + "_stride_head", sh)
-            if x in ("q", "k"):
-                setattr(c, "num_q_heads" if x == "q" else "num_kv_heads", H)
-            else:
-                _need(H == (c.num_q_heads if x == "q_out" else c.num_kv_heads), "%s does not go with the others" % x)
+        first, name = (q, "q") if q is not None else (k, "k")
+        dtype, tokens, head_dim = _dtype(first, name), first.shape[0], first.shape[-1]
+        least, bits = head_dim, 0                          # the shortest stride, and all strides' bits
+
+        def part(t, name, heads=None):
+            nonlocal least, bits
+            T, H, d, st, sh = _rows(t, name)
+            if t.dtype is not first.dtype or T != tokens or d != head_dim or heads not in (None, H):
+                raise ValueError("%s does not go with the others" % name)
+            least, bits = min(least, st, sh), bits | st | sh
+            return H, st, sh
+
+        Hq, q_st, q_sh = part(q, "q") if q is not None else (0, 0, 0)
+        Hkv, k_st, k_sh = part(k, "k") if k is not None else (0, 0, 0)
+        _, qo_st, qo_sh = part(q_out, "q_out", Hq) if q_out is not None else (Hq, q_st, q_sh)
+        _, ko_st, ko_sh = part(k_out, "k_out", Hkv) if k_out is not None else (Hkv, k_st, k_sh)
+        self.c = c = stem_rotary_shape(dtype, tokens, Hq, Hkv, head_dim, int(rotary_dim), LAYOUTS[layout], q_st, q_sh, k_st, k_sh,
+                                       qo_st, qo_sh, ko_st, ko_sh)
+        self.usable = least >= head_dim and not bits & 7   # what the library asks of strides
         self.q, self.k = _seen(q), _seen(k)
         self.q_out = _seen(q_out) if q_out is not None else self.q
         self.k_out = _seen(k_out) if k_out is not None else self.k
-        self.tokens, self.pairs = c.tokens, c.rotary_dim // 2
+        self.tokens, self.pairs = tokens, c.rotary_dim // 2
         self.ref = ctypes.byref(c)
 
     @classmethod
@@ -221,14 +227,12 @@ def usable_rows(t: torch.Tensor) -> bool:
 
 def need_usable_rows(shape: RotaryShape, *rows: Optional[torch.Tensor]) -> None:
     """What the library asks of the rows of a call beyond their sizes: whole 16 bytes, and no row within another."""
-    c, at = shape.c, 0
-    strides = [c.k_stride_token, c.k_stride_head]
-    if c.num_q_heads > 0:
-        strides += (c.q_stride_token, c.q_stride_head, c.q_out_stride_token, c.q_out_stride_head)
+    at = 0
     for t in rows:
-        at |= 0 if t is None else t.data_ptr()
-    if at & 15 or min(strides) < c.head_dim or any(x & 7 for x in strides):
-        raise ValueError("rows have to begin at whole 16 bytes, %d or more elements apart" % c.head_dim)
+        if t is not None:
+            at |= t.data_ptr()
+    if at & 15 or not shape.usable:
+        raise ValueError("rows have to begin at whole 16 bytes, %d or more elements apart" % shape.c.head_dim)
 
 
 class PageShape:
