@@ -143,7 +143,9 @@ def _whole(t: Optional[torch.Tensor], n: int, name: str, dev: int, dtype: torch.
 def _lines(t: Optional[torch.Tensor], n: int, each: int, name: str, dev: int, dtype: torch.dtype = torch.int32) -> int:
     """Address of a contiguous tensor of n lines (or more) of `each` numbers; one of another number of dimensions than two is
     taken for these lines one after the other."""
-    if t is None or t.dtype is not dtype or t.numel() < n * each or not t.is_contiguous() or t.dim() == 2 and t.size(1) != each:
+    s = () if t is None else t.shape
+    fit = s[0] >= n and s[1] == each if len(s) == 2 else len(s) > 0 and t.numel() >= n * each
+    if not fit or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError("%s has to be contiguous %s of at least %d lines of %d" % (name, dtype, n, each))
     if t.get_device() != dev:
         raise ValueError("%s is not on the current device" % name)
@@ -275,6 +277,7 @@ class TableShape:
                  position_offset: int = 0, max_new: int = 0):
         self.c = stem_table_shape(int(requests), int(page_size), int(num_pages), int(pages_per_request), int(token_capacity),
                                   int(position_offset), int(max_new))
+        self.sizes = int(requests), int(num_pages), int(pages_per_request), int(token_capacity)     # what its tensors go by
         self.ref = ctypes.byref(self.c)
 
 
@@ -288,14 +291,14 @@ def stem_block_table(shape: TableShape, past_lens: torch.Tensor, new_lens: Optio
                      ring: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, ring_state_out: torch.Tensor,
                      cu_new: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, status: torch.Tensor,
                      workspace: torch.Tensor) -> None:
-    (dev, stream), c = _here(), shape.c
-    R = c.requests
+    dev, stream = _here()
+    R, N, W, T = shape.sizes
     _check(lib().stem_block_table(
         shape.ref, _whole(past_lens, R, "past_lens", dev), None if new_lens is None else _whole(new_lens, R, "new_lens", dev),
-        _whole(ring_state, 2, "ring_state", dev), _whole(ring, c.num_pages, "ring", dev),
-        _lines(table, R, c.pages_per_request, "table", dev), _whole(lens, R, "lens", dev),
+        _whole(ring_state, 2, "ring_state", dev), _whole(ring, N, "ring", dev),
+        _lines(table, R, W, "table", dev), _whole(lens, R, "lens", dev),
         _whole(ring_state_out, 2, "ring_state_out", dev), _whole(cu_new, R + 1, "cu_new", dev),
-        _whole(positions, c.token_capacity, "positions", dev), _whole(slots, c.token_capacity, "slots", dev),
+        _whole(positions, T, "positions", dev), _whole(slots, T, "slots", dev),
         _whole(status, 4, "status", dev), _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(),
         stream), "stem_block_table")
 
@@ -325,6 +328,7 @@ class PrefixShape:
             _need(int(max_suffix) == 0, "a suffix needs pages")
             c.requests = table if isinstance(table, int) else table.shape[0]
         self.q, self.prefix, self.pages = _seen(q), _seen(prefix_k), pages.seen if pages is not None else None
+        self.sizes = c.requests, c.pages_per_request, c.max_suffix > 0, Hq, T                        # what its tensors go by
         self.ref = ctypes.byref(c)
 
     @classmethod
@@ -350,14 +354,13 @@ def stem_prefix_attn_workspace_bytes(shape: PrefixShape) -> int:
 def stem_prefix_attn(shape: PrefixShape, q: torch.Tensor, prefix_k, prefix_v, k_pages, v_pages, table, lens,
                      cu_new: Optional[torch.Tensor], softmax_scale: float, out: torch.Tensor, lse: Optional[torch.Tensor],
                      workspace: torch.Tensor) -> None:
-    (dev, stream), c = _here(), shape.c
-    paged = c.max_suffix > 0
+    dev, stream = _here()
+    R, W, paged, Hq, T = shape.sizes
     _check(lib().stem_prefix_attn(
         shape.ref, _values(q, shape.q, "q", dev), _values(prefix_k, shape.prefix, "prefix_k", dev),
         _values(prefix_v, shape.prefix, "prefix_v", dev), _values(k_pages, shape.pages, "k_pages", dev) if paged else None,
         _values(v_pages, shape.pages, "v_pages", dev) if paged else None,
-        _lines(table, c.requests, c.pages_per_request, "table", dev) if paged else None,
-        _whole(lens, c.requests, "lens", dev) if paged else None,
-        None if cu_new is None else _whole(cu_new, c.requests + 1, "cu_new", dev), softmax_scale,
-        _values(out, shape.q, "out", dev), None if lse is None else _lines(lse, c.num_q_heads, c.tokens, "lse", dev, torch.float32),
+        _lines(table, R, W, "table", dev) if paged else None, _whole(lens, R, "lens", dev) if paged else None,
+        None if cu_new is None else _whole(cu_new, R + 1, "cu_new", dev), softmax_scale,
+        _values(out, shape.q, "out", dev), None if lse is None else _lines(lse, Hq, T, "lse", dev, torch.float32),
         _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(), stream), "stem_prefix_attn")
