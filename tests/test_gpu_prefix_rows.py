@@ -3,7 +3,10 @@ there are, and their requests are looked up in cu_new."""
 import pytest
 import torch
 
-from test_gpu_prefix_attn import BF, HF, Case
+from paper_2603_06274_amd import decode_binding as db
+
+import decode_util as du
+from test_gpu_prefix_attn import BF, DEV, HF, Case
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +51,24 @@ def test_few_rows_are_not_refused_for_a_large_bound():
     c = Case([40] * 64, [1] * 64, 2048, 32, 8, 64, seed=5)
     c.max_new = 4097
     c.check(*c.run())
+
+
+def test_launches_of_more_than_one_line():
+    """65536 requests of 32 KV heads: 2^21 workgroups of own keys.  (Their pages are shared, which reading does not mind.)"""
+    R, H, d, N, L = 65536, 32, 64, 300, 20
+    g = torch.Generator(device=DEV).manual_seed(9)
+    normal = lambda *s: torch.randn(*s, generator=g, device=DEV).to(BF)
+    q, pk, pv, kp, vp = normal(R, H, d), normal(L, H, d), normal(L, H, d), normal(N, 16, H, d), normal(N, 16, H, d)
+    table = torch.randint(0, N, (R, 1), generator=g, device=DEV, dtype=torch.int32)
+    lens = torch.randint(1, 7, (R,), generator=g, device=DEV, dtype=torch.int32)
+    shape = db.PrefixShape.from_tensors(q, pk, db.PageShape.from_tensors(kp, vp), table, 1, 16)
+    space = torch.full((db.stem_prefix_attn_workspace_bytes(shape),), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full_like(q, 9.0)
+    db.stem_prefix_attn(shape, q, pk, pv, kp, vp, table, lens, None, d ** -0.5, out, None, space)
+    assert not (out == 9.0).all(dim=2).any() and out.isfinite().all()
+    line = 2 ** 20 // H                                # requests of the first line
+    some = [0, 1, 7, 8, line - 9, line - 2, line - 1, line, line + 1, line + 8, R - 9, R - 2, R - 1, *range(100, R, 3001)]
+    for r in some:
+        k, v = (torch.cat([x, p[table[r, 0], :lens[r]]]).cpu().double() for x, p in ((pk, kp), (pv, vp)))
+        o, bound, _, _ = du.attention_rows(q[r].cpu().double(), k, v, d ** -0.5, BF)
+        assert ((out[r].cpu().double() - o).abs() <= bound).all(), r
