@@ -147,8 +147,8 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     const int64_t own_rows = s.max_new * G < rows ? s.max_new * G : rows;
     p.suffix_row_tile = own_rows <= 16 ? 16 : 64;
     p.suffix_row_tiles = (int32_t)((own_rows + p.suffix_row_tile - 1) / p.suffix_row_tile);
-    // By the rows that there are, not by what each request might have: max_new is a bound for the longest (a step that takes a prompt of 2048
-    // tokens beside 63 single ones has 131072 row tiles of 64 by the one count, 2175 by the other).
+    // By the rows that there are, not by what each request might have: max_new is a bound for the longest (a prompt of 2048 tokens beside 63
+    // single ones, four heads per KV head: 8192 row tiles by the one count, 195 by the other; 1490 and 1200 us behind 32K keys).
     const int64_t by_request = (int64_t)s.requests * p.suffix_row_tiles, by_rows = slot_before(s.requests, rows, p.suffix_row_tile);
     p.own_by_rows = by_request > by_rows;
     p.own_slots = p.own_by_rows ? by_rows : by_request;

@@ -89,5 +89,7 @@ __host__ __device__ inline int suffix_split_keys(int len, int splits) {
     const int each = (int)(((int64_t)len + splits - 1) / splits);
     return (each + 127) & ~127;
 }
+// and the number of parts that are not empty
+__host__ __device__ inline int suffix_parts(int len, int splits) { return len > 0 ? (len - 1) / suffix_split_keys(len, splits) + 1 : 0; }
 
 }  // namespace stem

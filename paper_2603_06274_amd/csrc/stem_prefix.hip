@@ -715,14 +715,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         }
     }
     const int g = h / a.G;
-    if (mine) {
-        const int len = suffix_len(a, r);
-        parts = a.prefix_splits;
-        if (len > 0) {
-            const int each = suffix_split_keys(len, a.suffix_splits);
-            parts += (len + each - 1) / each;
-        }
-    }
+    if (mine) parts = a.prefix_splits + suffix_parts(suffix_len(a, r), a.suffix_splits);
     const int64_t step = (int64_t)a.Hkv * a.rows, row = (int64_t)g * a.rows + (int64_t)(first + i) * a.G + (h - g * a.G);
     float m = kNone, l = 0.f;
     f32x4_t o = {0.f, 0.f, 0.f, 0.f};

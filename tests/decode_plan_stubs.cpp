@@ -2,6 +2,7 @@
 #include "stem_decode_common.h"
 
 extern "C" int stem_test_suffix_split_keys(int32_t len, int32_t splits) { return stem::suffix_split_keys(len, splits); }
+extern "C" int stem_test_suffix_parts(int32_t len, int32_t splits) { return stem::suffix_parts(len, splits); }
 
 static int units_there;
 static int there() { return units_there; }

@@ -109,3 +109,12 @@ def test_every_row_tile_has_a_slot(host, G, tile):
             assert before[x + 1] - before[x] >= -(-n * G // tile) and before[x + 1] > before[x]
         # and all of them within what a call of so many tokens, and any behind them, has
         assert before[-1] <= host.stem_test_slot_before(len(new), (cu[-1] + r.randint(0, 9)) * G, tile)
+
+
+@pytest.mark.parametrize("splits", [1, 2, 3, 63, 64])
+def test_parts_are_counted_within_32_bits(host, splits):
+    """As many as hold a key: the last of them begins before the length's end, and the next would not."""
+    for length in (0, 1, 127, 128, 129, 1000, 2 ** 24 + 1, 2 ** 30, 2 ** 30 + 1, 3 * 2 ** 29, MOST_SUFFIX):
+        keys, parts = host.stem_test_suffix_split_keys(length, splits), host.stem_test_suffix_parts(length, splits)
+        assert parts == -(-length // keys) if length else parts == 0
+        assert parts <= splits
