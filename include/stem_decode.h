@@ -174,7 +174,8 @@ int stem_prefix_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* hos
  * Exact softmax attention of every request's new tokens to the shared prefix and to the request's own tokens:
  *   out[t, h, :] = sum_u softmax_u( softmax_scale * <Q[t, h], K[u, g]> ) V[u, g],   g = h / (Hq / Hkv)
  * over the prefix_len rows of prefix_k, prefix_v [prefix_len, Hkv, d] and the request's rows j in the pages with
- * j <= lens[r] - n + i, where t is number i of the n new tokens of request r (which stand at the end of its lens[r] tokens).
+ * j <= lens[r] - n + i, where t is number i of the n new tokens of request r (which stand at the end of its lens[r] tokens; n
+ * counts the rows that there are).
  *   - lens is int32 [requests], table int32 [requests, pages_per_request], cu_new int32 [requests + 1]: request r's new tokens are
  *     the rows cu_new[r] .. cu_new[r + 1] - 1 of Q and O, as far as there are such rows.  cu_new ascends (where it does not, rows of
  *     O and lse hold nothing defined); NULL: one token each, then tokens = requests.  Rows of no request are left as they were, in O

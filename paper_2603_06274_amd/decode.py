@@ -32,7 +32,8 @@ class _Turn(torch.autograd.Function):
 
 class Rotary:
     """Rotary positions of heads of `head_dim` values, of which the first `rotary_dim` turn (None: all), in the "half" or
-    "interleaved" layout, with frequencies scaled for long contexts by one of decode_binding.SCALINGS (low, high: as stem_rotary_frequencies has them)."""
+    "interleaved" layout, with frequencies scaled for long contexts by one of decode_binding.SCALINGS (low, high: as
+    stem_rotary_frequencies has them)."""
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, theta: float = 10000.0, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, trained_length: float = 0.0, low: float = 1.0,
@@ -95,7 +96,8 @@ class PagedCache:
     """Keys and values of up to `requests` requests in `num_pages` pages of `page_size` tokens, at most `pages_per_request` each, with the
     block tables, lengths and free pages that go with them, all on the GPU.  `tokens` is the number of rows of a step's tensors: a step has
     at most that many new tokens.  `position_offset`: the position of a request's first token.  Where it is not given, the first
-    StemDecode with rotary positions that is made of the cache sets it to the length of its prefix; a cache that begins before that begins at 0."""
+    StemDecode with rotary positions that is made of the cache sets it to the length of its prefix; a cache that begins before that
+    begins at 0.  A cache is one layer's, and its books are its own: each layer of a model has one, and they all take the same steps."""
 
     def __init__(self, requests: int, num_pages: int, page_size: int, pages_per_request: int, num_kv_heads: int, head_dim: int,
                  tokens: Optional[int] = None, position_offset: Optional[int] = None, dtype: torch.dtype = torch.bfloat16, device="cuda"):
@@ -179,8 +181,8 @@ class PagedCache:
 class StemDecode:
     """Decoding steps of the requests of a PagedCache behind a prefix that they share: prefix_k, prefix_v [L, Hkv, d], its keys turned
     already, as StemPrefill leaves them.  With rotary positions, new tokens stand behind the prefix, at L and on, unless the cache was
-    made with a position_offset (for keys whose positions do not begin at 0).  One object is one sequence of steps: its buffers belong to one step at a time.  A step may be
-    captured into a graph and replayed."""
+    made with a position_offset (for keys whose positions do not begin at 0).  One object is one sequence of steps: its buffers
+    belong to one step at a time.  A step may be captured into a graph and replayed."""
 
     def __init__(self, prefix_k: torch.Tensor, prefix_v: torch.Tensor, num_q_heads: int, cache: PagedCache,
                  rotary: Optional[Rotary] = None, max_new: int = 1, softmax_scale: Optional[float] = None,
