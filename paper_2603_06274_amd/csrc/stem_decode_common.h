@@ -86,10 +86,12 @@ __host__ __device__ inline int64_t slot_before(int r, int64_t row, int tile) { r
 // Keys of a part of a request's own `len`, of which there are at most `splits`: whole 128s, so that short ones use few parts.  The
 // kernel that computes partial results and the one that joins them both ask here.
 __host__ __device__ inline int suffix_split_keys(int len, int splits) {
-    const int each = (int)(((int64_t)len + splits - 1) / splits);
-    return (each + 127) & ~127;
+    const uint32_t each = ((uint32_t)len + (uint32_t)splits - 1) / (uint32_t)splits;
+    return (int)((each + 127) & ~127u);
 }
 // and the number of parts that are not empty
-__host__ __device__ inline int suffix_parts(int len, int splits) { return len > 0 ? (len - 1) / suffix_split_keys(len, splits) + 1 : 0; }
+__host__ __device__ inline int suffix_parts(int len, int splits) {
+    return len > 0 ? (int)((uint32_t)(len - 1) / (uint32_t)suffix_split_keys(len, splits)) + 1 : 0;
+}
 
 }  // namespace stem

@@ -76,7 +76,7 @@ struct PrefixArgs {
     int32_t max_suffix, suffix_splits, suffix_row_tiles;
     int32_t table_row, page_shift, num_pages;
     int32_t prefix_groups, groups;                     // workgroups of the prefix, and with those of the own keys
-    bool own_by_rows, join_by_rows;                    // how the latter, and the rows that are joined, are counted: PrefixPlan
+    bool own_by_rows;                                  // how the latter are counted: PrefixPlan
     int64_t q_st, q_sh, p_st, p_sh, page_st, tok_st, head_st;
 };
 
@@ -110,8 +110,10 @@ __device__ __forceinline__ int last_at_most(int count, int64_t x, Key key) {
     const uint64_t below = __builtin_amdgcn_ballot_w64(lane < count && key(from + lane) <= x);
     return below ? from + 63 - __builtin_clzll(below) : -1;
 }
-// A launch's workgroups are numbered along lines of a grid that has more than one if there are very many.
-__device__ __forceinline__ int64_t group_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+// A launch's workgroups are numbered along lines of 2^20, of which a grid has more than one if there are very many.  (A constant: the grid's
+// size would be one more load that every workgroup waits for.)  There are at most 2^31 - 2^20, which whole lines do not bring beyond 2^31.
+constexpr int kLineBits = 20;
+__device__ __forceinline__ uint32_t group_number() { return (blockIdx.y << kLineBits) + blockIdx.x; }
 __device__ __forceinline__ int suffix_len(const PrefixArgs& a, int r) {
     return a.max_suffix > 0 ? min(max(a.lens[r], 0), a.max_suffix) : 0;
 }
@@ -610,9 +612,8 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     using PartO = Part<T, D, SO>;
     __shared__ __align__(1024) unsigned char lds[PartP::kLds > PartO::kLds ? PartP::kLds : PartO::kLds];
     __shared__ float2 wave_ml[SP::kRows * SP::KW > SO::kRows * SO::KW ? SP::kRows * SP::KW : SO::kRows * SO::KW];
-    const int64_t number = group_number();
-    if (number >= a.groups) return;
-    const int id = (int)number;
+    const int id = (int)group_number();
+    if (id >= a.groups) return;
     if (id < a.prefix_groups) {
         // row tiles of the same keys on one XCD (workgroup id modulo 8), one after the other: they share its L2
         const int x = id & 7, y = id >> 3, row_tile = y % a.row_tiles, combo = y / a.row_tiles * 8 + x;
@@ -632,7 +633,7 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     at /= a.Hkv;
     const int split = at % a.suffix_splits, slot = at / a.suffix_splits;
     int r, row_tile;
-    if (a.own_by_rows) {
+    if (__builtin_expect(a.own_by_rows, 0)) {
         auto before = [&](int x) { return slot_before(x, (int64_t)first_token(a, x) * a.G, SO::kRows); };
         r = last_at_most(a.requests, slot, before);
         if (r < 0) return;
@@ -678,26 +679,26 @@ __global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a
 // Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
 // at a time is asked for before any of it is used, as a row waits for memory and does next to nothing else.
 constexpr int kJoinThreads = 256;
-template <typename T, int D, int GROUPS>
+template <typename T, int D, int GROUPS, bool BY_ROWS>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
     constexpr int kLanes = D / 4, kRows = kJoinThreads / (kLanes * GROUPS), kAtOnce = 4;
     __shared__ f32x4_t group_o[GROUPS > 1 ? kJoinThreads : 1];
     __shared__ float2 group_ml[GROUPS > 1 ? kRows * GROUPS : 1];
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes % GROUPS, my_row = threadIdx.x / (kLanes * GROUPS);
-    const int64_t item = group_number() * kRows + my_row;
+    const uint32_t item0 = group_number() * kRows, item = item0 + my_row;   // (2^31 and less than a line's more)
     int r = 0, i = 0, h = 0, first = 0, n = 0, parts = 0;
     bool mine = false;                                 // whether the row is one of a request's
-    if (a.join_by_rows) {                              // token, head
+    if constexpr (BY_ROWS) {                           // token, head
         constexpr int kWaveRows = GROUPS > 1 ? 1 : 64 / kLanes;   // different rows of a wave
-        const int64_t item0 = GROUPS > 1 ? item : group_number() * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
+        const uint32_t wave0 = GROUPS > 1 ? item0 : item0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
         int known = -1, owner = -1;
 #pragma unroll
         for (int x = 0; x < kWaveRows; ++x) {
-            const int64_t token = (item0 + x) / a.Hq;
-            if (token >= a.tokens) break;
-            if (token != known) owner = last_at_most(a.requests, token, [&](int y) { return (int64_t)first_token(a, y); });
+            const uint32_t token = (wave0 + x) / (uint32_t)a.Hq;
+            if (token >= (uint32_t)a.tokens) break;
+            if ((int)token != known) owner = last_at_most(a.requests, token, [&](int y) { return (int64_t)first_token(a, y); });
             known = (int)token;
-            if (item == item0 + x) r = owner, i = known, h = (int)(item - token * a.Hq), mine = owner >= 0;
+            if (item == wave0 + x) r = owner, i = known, h = (int)(item - token * (uint32_t)a.Hq), mine = owner >= 0;
         }
         if (mine) {
             new_tokens(a, r, first, n);
@@ -705,10 +706,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
             mine = i < min(n, a.max_new);
         }
     } else {                                           // request, new token, head
-        const int64_t per_request = (int64_t)a.max_new * a.Hq, request = item / per_request;
+        const uint32_t per_request = (uint32_t)a.max_new * a.Hq, request = item / per_request;
         const int rest = (int)(item - request * per_request);
         i = rest / a.Hq, h = rest - i * a.Hq;
-        if (request < a.requests) {
+        if (request < (uint32_t)a.requests) {
             r = (int)request;
             new_tokens(a, r, first, n);
             mine = i < n;
@@ -785,7 +786,8 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
     constexpr int kGroups = 4 * kJoinThreads / D;
     const bool many = p.prefix_splits + p.suffix_splits > 4;
     // (a line of a grid has less than 2^32 threads, and where there are lines each begins with a workgroup of XCD 0)
-    auto grid_of = [](int64_t n) { return n <= 1 << 20 ? dim3((unsigned)n) : dim3(1 << 20, (unsigned)((n + (1 << 20) - 1) >> 20)); };
+    constexpr int64_t kLine = 1 << kLineBits;
+    auto grid_of = [](int64_t n) { return n <= kLine ? dim3((unsigned)n) : dim3((unsigned)kLine, (unsigned)((n + kLine - 1) >> kLineBits)); };
     const dim3 grid = grid_of(p.groups), joins = grid_of(many ? p.join_rows : (p.join_rows + kGroups - 1) / kGroups);
     if (p.groups > 0) {
 #define STEM_PREFIX_LAUNCH(SP, SO) \
@@ -801,8 +803,12 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
 #undef STEM_PREFIX_LAUNCH
         if (const int st = check_launch()) return st;
     }
-    if (many) hipLaunchKernelGGL((join_kernel<T, D, kGroups>), joins, dim3(kJoinThreads), 0, stream, a);
-    else hipLaunchKernelGGL((join_kernel<T, D, 1>), joins, dim3(kJoinThreads), 0, stream, a);
+#define STEM_JOIN_LAUNCH(GROUPS, BY_ROWS) hipLaunchKernelGGL((join_kernel<T, D, GROUPS, BY_ROWS>), joins, dim3(kJoinThreads), 0, stream, a)
+    if (many && p.join_by_rows) STEM_JOIN_LAUNCH(kGroups, true);
+    else if (many) STEM_JOIN_LAUNCH(kGroups, false);
+    else if (p.join_by_rows) STEM_JOIN_LAUNCH(1, true);
+    else STEM_JOIN_LAUNCH(1, false);
+#undef STEM_JOIN_LAUNCH
     return check_launch();
 }
 
@@ -828,7 +834,7 @@ int launch_prefix_attn(const PrefixCall& c, hipStream_t stream) {
     a.page_shift = s.max_suffix > 0 ? __builtin_ctz(s.pages.page_size) : 0;
     a.num_pages = s.pages.num_pages;
     a.prefix_groups = (int32_t)p.prefix_groups, a.groups = (int32_t)p.groups;
-    a.own_by_rows = p.own_by_rows, a.join_by_rows = p.join_by_rows;
+    a.own_by_rows = p.own_by_rows;
     a.q_st = s.q_stride_token, a.q_sh = s.q_stride_head, a.p_st = s.prefix_stride_token, a.p_sh = s.prefix_stride_head;
     a.page_st = s.pages.stride_page, a.tok_st = s.pages.stride_token, a.head_st = s.pages.stride_head;
     if (s.dtype == STEM_BF16) {
