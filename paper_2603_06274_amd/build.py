@@ -17,7 +17,7 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libstem_hip.so")
 
 SOURCES = ["stem_api.cpp", "stem_pool.hip", "stem_scores.hip", "stem_select.hip", "stem_attn.hip", "stem_static.hip",
-           "stem_decode_api.cpp", "stem_rotary.hip", "stem_table.hip", "stem_prefix.hip"]
+           "stem_decode_api.cpp", "stem_rotary.hip", "stem_table.hip", "stem_prefix.hip", "stem_norm_api.cpp", "stem_norm.hip"]
 
 # instantiations of sparse_attn_kernel: block sizes 64 and 128 times head sizes 64, 128 and 256 times the two numbers of
 # queries per wave

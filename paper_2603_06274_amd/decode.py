@@ -71,6 +71,9 @@ class Rotary:
         db.stem_rotary(shape, q, k, positions, self.turns, self.attention_factor, q_out, k_out, backward)
         return q_out, k_out
 
+    def _append(self, shape: db.RotaryShape, pages: db.PageShape, q, k, v, positions, slots, q_out, k_pages, v_pages) -> None:
+        db.stem_rotary_append(shape, pages, q, k, v, positions, slots, self.turns, self.attention_factor, q_out, k_pages, v_pages)
+
     def apply(self, q, k, positions: torch.Tensor, q_out=None, k_out=None):
         """q [T, Hq, d] and k [T, Hkv, d] (either may be None) turned by positions int32 [T]; into new tensors unless q_out and
         k_out are given, which may be q and k themselves.  New tensors carry q's and k's gradients."""
@@ -174,8 +177,7 @@ class PagedCache:
         return q_out
 
     def _write(self, shape: db.RotaryShape, rotary: Rotary, q, k, v, q_out) -> None:
-        db.stem_rotary_append(shape, self.pages, q, k, v, self.positions, self.slots, rotary.turns, rotary.attention_factor, q_out,
-                              self.k_pages, self.v_pages)
+        rotary._append(shape, self.pages, q, k, v, self.positions, self.slots, q_out, self.k_pages, self.v_pages)
 
 
 class StemDecode:
