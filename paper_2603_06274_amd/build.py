@@ -17,7 +17,8 @@ OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libstem_hip.so")
 
 SOURCES = ["stem_api.cpp", "stem_pool.hip", "stem_scores.hip", "stem_select.hip", "stem_attn.hip", "stem_static.hip",
-           "stem_decode_api.cpp", "stem_rotary.hip", "stem_table.hip", "stem_prefix.hip", "stem_norm_api.cpp", "stem_norm.hip"]
+           "stem_decode_api.cpp", "stem_rotary.hip", "stem_table.hip", "stem_prefix.hip", "stem_norm_api.cpp", "stem_norm.hip",
+           "stem_tree_api.cpp", "stem_tree.hip", "stem_tree_attn.hip"]
 
 # instantiations of sparse_attn_kernel: block sizes 64 and 128 times head sizes 64, 128 and 256 times the two numbers of
 # queries per wave
@@ -33,7 +34,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-I" + os.path.
 # was copied on the common path too, and the B = 128, d = 128 kernel spilled 79 registers.  Results of the matrix instructions
 # that the compiler places stay in vector registers also in a kernel that uses accumulator registers by hand (head size 256).
 FLAGS = {"stem_attn.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions", "-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "stem_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "stem_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "stem_tree_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc() -> str:

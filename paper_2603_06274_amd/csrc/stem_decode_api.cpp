@@ -28,7 +28,7 @@ static int check_table(const stem_table_shape* s) {
     return STEM_OK;
 }
 
-static int check_prefix(const stem_prefix_shape* s) {
+int check_prefix(const stem_prefix_shape* s) {
     if (!s) return STEM_ERR_INVALID_ARG;
     if (s->dtype != STEM_BF16 && s->dtype != STEM_FP16) return STEM_ERR_INVALID_ARG;
     if (s->num_q_heads <= 0 || s->num_kv_heads <= 0 || s->num_q_heads % s->num_kv_heads) return STEM_ERR_INVALID_ARG;
@@ -57,7 +57,7 @@ static int check_prefix(const stem_prefix_shape* s) {
     return STEM_OK;
 }
 
-int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
+int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)(), bool tree) {
     const int units_here = units();
     if (units_here <= 0) return STEM_ERR_HIP;
     const int64_t G = s.num_q_heads / s.num_kv_heads, rows = s.tokens * G;
@@ -88,7 +88,8 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
         p.prefix_splits = (int32_t)((tiles + best_each - 1) / best_each);
     }
     const int64_t own_rows = s.max_new * G < rows ? s.max_new * G : rows;
-    p.suffix_row_tile = own_rows <= 16 ? 16 : 64;
+    p.suffix_row_tile = own_rows <= 16 ? 16 : !tree || own_rows <= 64 ? 64 : 128;
+    p.suffix_least = 128;
     p.suffix_row_tiles = (int32_t)((own_rows + p.suffix_row_tile - 1) / p.suffix_row_tile);
     // By the rows that there are, not by what each request might have: max_new is a bound for the longest (a prompt of 2048 tokens beside 63
     // single ones, four heads per KV head: 8192 row tiles by the one count, 195 by the other; 1490 and 1200 us behind 32K keys).
@@ -121,6 +122,21 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)()) {
     if (p.bytes == 0) p.bytes = 256;
     *plan = p;
     return STEM_OK;
+}
+
+int prepare_prefix(PrefixCall& c, size_t workspace_bytes, bool tree) {
+    const stem_prefix_shape& s = c.shape;
+    if (!c.q || !aligned(c.q, 16) || !c.out || !aligned(c.out, 16) || c.q == c.out || !aligned(c.lse, 4)) return STEM_ERR_INVALID_ARG;
+    if (s.prefix_len > 0 && (!c.prefix_k || !aligned(c.prefix_k, 16) || !c.prefix_v || !aligned(c.prefix_v, 16)))
+        return STEM_ERR_INVALID_ARG;
+    if (s.max_suffix > 0) {
+        if (!c.table || !aligned(c.table, 4) || !c.lens || !aligned(c.lens, 4)) return STEM_ERR_INVALID_ARG;
+        if (s.pages.num_pages > 0 && (!c.k_pages || !aligned(c.k_pages, 16) || !c.v_pages || !aligned(c.v_pages, 16)))
+            return STEM_ERR_INVALID_ARG;
+    }
+    if (!c.workspace || !aligned(c.workspace, 16)) return STEM_ERR_INVALID_ARG;
+    if (const int st = prefix_plan(s, &c.plan, compute_units, tree)) return st;
+    return workspace_bytes < c.plan.bytes ? STEM_ERR_WORKSPACE : STEM_OK;
 }
 
 }  // namespace stem
@@ -253,18 +269,8 @@ int stem_prefix_attn(const stem_prefix_shape* shape, const void* q, const void* 
     if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.f)) return STEM_ERR_INVALID_ARG;
     if (!aligned(cu_new, 4) || (!cu_new && s.tokens != s.requests)) return STEM_ERR_INVALID_ARG;
     if (s.tokens == 0) return STEM_OK;
-    if (!q || !aligned(q, 16) || !out || !aligned(out, 16) || q == out || !aligned(lse, 4)) return STEM_ERR_INVALID_ARG;
-    if (s.prefix_len > 0 && (!prefix_k || !aligned(prefix_k, 16) || !prefix_v || !aligned(prefix_v, 16)))
-        return STEM_ERR_INVALID_ARG;
-    if (s.max_suffix > 0) {
-        if (!table || !aligned(table, 4) || !lens || !aligned(lens, 4)) return STEM_ERR_INVALID_ARG;
-        if (s.pages.num_pages > 0 && (!k_pages || !aligned(k_pages, 16) || !v_pages || !aligned(v_pages, 16)))
-            return STEM_ERR_INVALID_ARG;
-    }
-    if (!workspace || !aligned(workspace, 16)) return STEM_ERR_INVALID_ARG;
     PrefixCall call = {s, {}, q, prefix_k, prefix_v, k_pages, v_pages, table, lens, cu_new, softmax_scale, out, lse, workspace};
-    if (const int st = prefix_plan(s, &call.plan)) return st;
-    if (workspace_bytes < call.plan.bytes) return STEM_ERR_WORKSPACE;
+    if (const int st = prepare_prefix(call, workspace_bytes, false)) return st;
     return launch_prefix_attn(call, static_cast<hipStream_t>(hip_stream));
 }
 

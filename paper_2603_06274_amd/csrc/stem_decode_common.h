@@ -48,6 +48,7 @@ struct PrefixPlan {
     int32_t suffix_row_tile;
     int32_t suffix_row_tiles;  // per request: ceil(max_new * G / suffix_row_tile)
     int32_t suffix_splits;     // 0 if there are no pages
+    int32_t suffix_least;      // keys of a part of the own ones at least
     // Pairs (request, row tile) per KV head and part of the own keys: suffix_row_tiles for every request or, where that is more,
     // rows / tile for all together and one for each (own_by_rows: slot_before says whose a slot is).
     int64_t own_slots;
@@ -61,7 +62,9 @@ struct PrefixPlan {
     size_t bytes;
 };
 // units: where the number of compute units comes from
-int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)() = compute_units);
+// tree: a call of stem_tree_attn
+int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)() = compute_units, bool tree = false);
+int check_prefix(const stem_prefix_shape* s);
 
 struct PrefixCall {
     stem_prefix_shape shape;
@@ -73,6 +76,8 @@ struct PrefixCall {
     float* lse;
     void* workspace;
 };
+// What is left to check of a call with such a shape and with tokens, and its plan.
+int prepare_prefix(PrefixCall& call, size_t workspace_bytes, bool tree);
 int launch_prefix_attn(const PrefixCall& call, hipStream_t stream);
 
 // Most own tokens of a request.  The kernel counts keys in 32 bits: parts are rounded up to 128 keys and there are 64 at most, and a
@@ -83,15 +88,16 @@ constexpr int32_t kMaxSuffix = 0x7fffffff - 0x3fff;
 // before, which is at least as many as these have tiles.  (floor(b / t) + 1 - floor(a / t) is whole and more than (b - a) / t.)
 __host__ __device__ inline int64_t slot_before(int r, int64_t row, int tile) { return row / tile + r; }
 
-// Keys of a part of a request's own `len`, of which there are at most `splits`: whole 128s, so that short ones use few parts.  The
-// kernel that computes partial results and the one that joins them both ask here.
-__host__ __device__ inline int suffix_split_keys(int len, int splits) {
+// Keys of a part of a request's own `len`, of which there are at most `splits`: whole 128s and `least` at least, so that short ones use few
+// parts.  The kernel that computes partial results and the one that joins them both ask here.
+__host__ __device__ inline int suffix_split_keys(int len, int splits, int least = 128) {
     const uint32_t each = ((uint32_t)len + (uint32_t)splits - 1) / (uint32_t)splits;
-    return (int)((each + 127) & ~127u);
+    const int keys = (int)((each + 127) & ~127u);
+    return keys > least ? keys : least;
 }
 // and the number of parts that are not empty
-__host__ __device__ inline int suffix_parts(int len, int splits) {
-    return len > 0 ? (int)((uint32_t)(len - 1) / (uint32_t)suffix_split_keys(len, splits)) + 1 : 0;
+__host__ __device__ inline int suffix_parts(int len, int splits, int least = 128) {
+    return len > 0 ? (int)((uint32_t)(len - 1) / (uint32_t)suffix_split_keys(len, splits, least)) + 1 : 0;
 }
 
 }  // namespace stem

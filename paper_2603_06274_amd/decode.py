@@ -7,6 +7,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import decode_binding as db
+from . import tree_binding as tb
 
 
 class _Turn(torch.autograd.Function):
@@ -124,6 +125,11 @@ class PagedCache:
         self.ring = torch.arange(num_pages, dtype=torch.int32, device=device)
         self.ring_state = torch.tensor([0, num_pages], dtype=torch.int32, device=device)
         self.workspace = torch.empty(db.stem_block_table_workspace_bytes(self.shape), dtype=torch.uint8, device=device)
+        # of what is kept of drafts: see accept
+        self.accepted, self.accept_status = whole(self.requests), whole(2)
+        self.path = whole(max(self.tokens, 1), value=-1)
+        self.next_ids = {t: torch.full((self.requests,), -1, dtype=t, device=device) for t in (torch.int32, torch.int64)}
+        self._step_open = False                            # whether there is a step of which nothing has been accepted yet
 
     def advance(self, new_lens: Optional[torch.Tensor] = None, max_new: int = 0) -> None:
         """Room for a step: new_lens int32 [requests] new tokens (None: one each; negative: the request has finished and its pages
@@ -131,6 +137,7 @@ class PagedCache:
         there is no room changes none of the first two, has no tokens and says so in status (see refused)."""
         self.shape.c.max_new = max_new
         self._offset_open = False
+        self._step_open = True
         db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
                             self.cu_new, self.positions, self.slots, self.status, self.workspace)
 
@@ -151,6 +158,31 @@ class PagedCache:
         """What the last step lacked: pages; requests with unusable lengths, too long for their row or of more new tokens than allowed;
         tokens beyond the step's rows; room for pages given back.  Waits for the GPU."""
         return tuple(self.status.tolist())
+
+    def accept(self, parents: torch.Tensor, draft_ids: torch.Tensor, target_ids: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """What is kept of the last step's new tokens, of which parents int32 [tokens] says behind which number of its request's new ones each
+        was drafted: a request's first one, and behind a kept one the draft that is the model's own choice there.  draft_ids and target_ids
+        (int32 or int64 [tokens]): the token in each row, and the model's choice behind it.  Brings lengths and free pages up to date and
+        moves the kept tokens' keys and values up; once per step.  Returns (accepted int32 [requests], path int32 [tokens], next_ids
+        [requests]), as stem_tree_accept has them, in buffers of the cache.  What cannot be done changes nothing and shows in
+        accept_refused."""
+        if not self._step_open:
+            raise RuntimeError("there is no step of which anything could be accepted")
+        c, ids = self.shape.c, draft_ids.dtype
+        if ids not in self.next_ids:
+            raise ValueError("token numbers are int32 or int64")
+        max_new = min(c.max_new, tb.STEM_MAX_TREE) if c.max_new > 0 else tb.STEM_MAX_TREE
+        shape = tb.AcceptShape(c.requests, self.tokens, max_new, c.page_size, c.num_pages, c.pages_per_request)
+        tb.stem_tree_accept(shape, parents, draft_ids, target_ids, self.cu_new, self.lens, self.ring_state, self.ring, self.table, self.lens,
+                            self.ring_state, self.accepted, self.path, self.next_ids[ids], self.accept_status, self.workspace)
+        self._step_open = False
+        tb.stem_tree_commit(shape, self.pages, self.path, self.slots, self.cu_new, self.k_pages, self.v_pages)
+        return self.accepted, self.path, self.next_ids[ids]
+
+    def accept_refused(self) -> Tuple[int, int]:
+        """Why the last accept was refused, if it was: requests with unusable numbers of tokens; room for pages given back.  Waits for the
+        GPU."""
+        return tuple(self.accept_status.tolist())
 
     def _rows_shape(self, rotary: Rotary, q, k, v, q_out) -> db.RotaryShape:
         """The shape of a step's rows.  Raises unless they go with the cache and with each other."""
@@ -184,11 +216,12 @@ class StemDecode:
     """Decoding steps of the requests of a PagedCache behind a prefix that they share: prefix_k, prefix_v [L, Hkv, d], its keys turned
     already, as StemPrefill leaves them.  With rotary positions, new tokens stand behind the prefix, at L and on, unless the cache was
     made with a position_offset (for keys whose positions do not begin at 0).  One object is one sequence of steps: its buffers
-    belong to one step at a time.  A step may be captured into a graph and replayed."""
+    belong to one step at a time.  A step may be captured into a graph and replayed.  With `tree`, a step's new tokens may be drafts that
+    form trees (max_new at most STEM_MAX_TREE): see step, and PagedCache.accept."""
 
     def __init__(self, prefix_k: torch.Tensor, prefix_v: torch.Tensor, num_q_heads: int, cache: PagedCache,
                  rotary: Optional[Rotary] = None, max_new: int = 1, softmax_scale: Optional[float] = None,
-                 want_lse: bool = False):
+                 want_lse: bool = False, tree: bool = False):
         d, dev, dtype = prefix_k.shape[2], prefix_k.device, prefix_k.dtype
         self.prefix_k, self.prefix_v, self.cache = prefix_k, prefix_v, cache
         self.turned = Turned(True)
@@ -207,24 +240,47 @@ class StemDecode:
             raise ValueError("the prefix and the positions have to be on the cache's device")
         if num_q_heads + 2 * prefix_k.shape[1] > db.MAX_HEADS:
             raise ValueError("a token has at most %d heads in all" % db.MAX_HEADS)
-        self.workspace = torch.empty(db.stem_prefix_attn_workspace_bytes(self.shape), dtype=torch.uint8, device=dev)
+        space = db.stem_prefix_attn_workspace_bytes(self.shape)
+        self.masks = self.tree_status = None
+        if tree:
+            space = max(space, tb.stem_tree_attn_workspace_bytes(self.shape))
+            self.masks = torch.zeros(cache.tokens, tb.mask_words(max_new), dtype=torch.int64, device=dev)
+            self.tree_status = torch.zeros(1, dtype=torch.int32, device=dev)      # parents that are none, over all steps
+        self.workspace = torch.empty(space, dtype=torch.uint8, device=dev)
         if rotary is not None:
             cache.begin_behind(prefix_k.shape[0])
 
-    def attend(self) -> torch.Tensor:
-        """Attention of self.q's rows, whose keys and values are in the cache, to the prefix and to their requests' tokens."""
+    def attend(self, tree: bool = False) -> torch.Tensor:
+        """Attention of self.q's rows, whose keys and values are in the cache, to the prefix and to their requests' tokens; with `tree`, of
+        the new ones to those in self.masks."""
         self.turned.need()
         c = self.cache
+        if tree:
+            tb.stem_tree_attn(self.shape, self.q, self.prefix_k, self.prefix_v, c.k_pages, c.v_pages, c.table, c.lens, c.cu_new, self.masks,
+                              self.softmax_scale, self.out, self.lse, self.workspace)
+            return self.out
         db.stem_prefix_attn(self.shape, self.q, self.prefix_k, self.prefix_v, c.k_pages, c.v_pages, c.table, c.lens, c.cu_new,
                             self.softmax_scale, self.out, self.lse, self.workspace)
         return self.out
 
-    def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, new_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    def step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, new_lens: Optional[torch.Tensor] = None,
+             parents: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One step: room for the new tokens, their keys and values into the cache, their attention.  Rows as in PagedCache.append; a
-        step with more than max_new tokens of a request is one without room.  Returns self.out, whose rows behind the last new token
-        keep what they held."""
+        step with more than max_new tokens of a request is one without room.  With parents int32 [tokens] (for an object made with `tree`),
+        each new token was drafted behind the one of that number among its request's new ones (-1: behind the earlier tokens), stands
+        one position behind it and sees it and what that one sees.  Returns self.out, whose rows behind the last new token keep what they
+        held."""
         self.turned.need()
-        shape = self.cache._rows_shape(self.rotary, q, k, v, self.q)      # (what it refuses leaves the cache as it was)
-        self.cache.advance(new_lens, self.max_new)
-        self.cache._write(shape, self.rotary, q, k, v, self.q)
-        return self.attend()
+        c = self.cache
+        shape = c._rows_shape(self.rotary, q, k, v, self.q)      # (what it refuses leaves the cache as it was)
+        if parents is not None:
+            if self.masks is None:
+                raise ValueError("trees need an object that was made with tree=True")
+            if parents.dtype != torch.int32 or parents.numel() < c.tokens or not parents.is_contiguous() or parents.device != c.lens.device:
+                raise ValueError("parents have to be contiguous int32 of at least %d elements, on the cache's device" % c.tokens)
+        c.advance(new_lens, self.max_new)
+        if parents is not None:
+            tree = tb.TreeShape(c.requests, c.tokens, self.max_new, c.shape.c.position_offset)
+            tb.stem_tree_masks(tree, parents, c.lens, c.cu_new, c.positions, self.masks, self.tree_status)
+        c._write(shape, self.rotary, q, k, v, self.q)
+        return self.attend(parents is not None)

@@ -127,10 +127,11 @@ class StemPrefill:
                                 self.indices, self.kmax, debug_scores, self.workspace)
 
     def decode(self, cache: PagedCache, sequence: int = 0, max_new: int = 1, want_lse: bool = False,
-               rotary: Optional[Rotary] = None) -> StemDecode:
+               rotary: Optional[Rotary] = None, tree: bool = False) -> StemDecode:
         """Decoding steps of the cache's requests behind one of the pre-filled sequences, with this layer's rotary positions and scale.
         `rotary`: the positions of queries and keys that were turned before the call (a chunked prompt's, for one); without any, new
-        rows are taken as they come.  With rotary positions, the cache's position_offset has to be the sequence's length (or not given)."""
+        rows are taken as they come.  With rotary positions, the cache's position_offset has to be the sequence's length (or not given).  `tree`: see
+        StemDecode."""
         if rotary is not None and self.rotary is not None and rotary is not self.rotary:
             raise ValueError("the keys were turned by other positions")
         rotary = rotary if rotary is not None else self.rotary
@@ -140,7 +141,7 @@ class StemPrefill:
         if rotary is not None and cache.offset_given and cache.shape.c.position_offset != rows.stop - rows.start:
             raise ValueError("the cache's positions begin at %d, behind a sequence of %d tokens" %
                              (cache.shape.c.position_offset, rows.stop - rows.start))
-        decode = StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, rotary, max_new, self.softmax_scale, want_lse)
+        decode = StemDecode(self.k[rows], self.v[rows], self.q.shape[1], cache, rotary, max_new, self.softmax_scale, want_lse, tree)
         decode.turned = self.turned
         return decode
 
