@@ -101,8 +101,19 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)(), bo
     p.suffix_splits = 0;
     if (s.max_suffix > 0 && rows > 0) {
         const int64_t others = p.own_slots * s.num_kv_heads;
-        const int64_t wanted = (units_here + others - 1) / others;   // (half as many as fit at a time: 52.0, twice as many 53.9 us with 32K keys)
-        const int64_t tiles = ((int64_t)s.max_suffix + 255) / 256;
+        // (half as many as fit at a time: 52.0, twice as many 53.9 us with 32K keys)
+        int64_t wanted = (units_here + others - 1) / others, tiles = ((int64_t)s.max_suffix + 255) / 256;
+        if (tree) {
+            // Own keys of trees are much of the work, and of very different lengths: parts for two to four rounds of workgroups, so that the
+            // longest request's do not end long after the others'.  Of 128 rows, 512 keys at least: a part's results are 512 bytes a row on their
+            // way out and in, its keys as many each.  Us for parts of 1 / 2 / 4 / 8 workgroups per CU: 16 requests of up to 32 drafts and
+            // 32768 tokens, 32 / 8 heads of 128: 512 / 296 / 265 / 261; 64 of 16 and 8192: 246 / 246 / 242 / 244; 32 of 4 and 16384 (16 rows): 221 /
+            // 226 / 197 / 203; d = 64, 16 of 32 and 16384: 221 / 125 / 105 / 95; d = 256, 8 of 32 and 16384: 122 / 105 / 112 / 112.
+            const int per_cu = s.head_dim == 256 ? 2 : p.suffix_row_tile == 128 ? 8 : 4;
+            p.suffix_least = p.suffix_row_tile == 128 ? 512 : 128;
+            wanted = ((int64_t)per_cu * units_here + others - 1) / others;
+            tiles = ((int64_t)s.max_suffix + p.suffix_least - 1) / p.suffix_least;
+        }
         p.suffix_splits = (int32_t)(wanted < tiles ? wanted : tiles);
         if (p.suffix_splits > 64) p.suffix_splits = 64;
     }
