@@ -98,7 +98,8 @@ int stem_tree_accept(const stem_accept_shape* shape, const int32_t* parents, con
  * Rows of K and V of kept tokens move up: for k = 0, 1, .. the row at slots[cu_new[r] + path[cu_new[r] + k]] goes to slots[cu_new[r] + k],
  * for each request until its path's first entry that is no number of a new token.  path ascends strictly.  slots are those of the step's
  * new tokens as stem_block_table left them (before lens_out took lens' place); tokens without a place (-1) stay out.  Of the shape,
- * requests, tokens and max_new count.  The pages have num_kv_heads heads of head_dim values (a multiple of 8, at most STEM_MAX_HEAD_DIM) of dtype.
+ * requests, tokens and max_new count.  The pages have num_kv_heads heads of head_dim values (a multiple of 8, at most STEM_MAX_HEAD_DIM) of dtype,
+ * 64 MiB per token at most (STEM_ERR_UNSUPPORTED).
  */
 int stem_tree_commit(const stem_accept_shape* shape, const stem_pages* pages, int32_t dtype, int32_t num_kv_heads, int32_t head_dim,
                      const int32_t* path, const int32_t* slots, const int32_t* cu_new, void* k_pages, void* v_pages, void* hip_stream);

@@ -101,14 +101,15 @@ int stem_tree_commit(const stem_accept_shape* shape, const stem_pages* pages, in
     if (const int st = check_tree_sizes(shape->requests, shape->tokens, shape->max_new)) return st;
     if (dtype != STEM_BF16 && dtype != STEM_FP16 && dtype != STEM_FP32) return STEM_ERR_INVALID_ARG;
     if (num_kv_heads < 1 || head_dim < 1 || head_dim % 8) return STEM_ERR_INVALID_ARG;
-    if (num_kv_heads > 65535 || head_dim > STEM_MAX_HEAD_DIM) return STEM_ERR_UNSUPPORTED;
+    const int32_t bytes = dtype == STEM_FP32 ? 4 : 2;
+    // (a token's rows of K and V are one line of a grid, in workgroups of 4 KiB)
+    if (head_dim > STEM_MAX_HEAD_DIM || (int64_t)num_kv_heads * head_dim * bytes > 1 << 26) return STEM_ERR_UNSUPPORTED;
     if (const int st = check_pages(*pages, head_dim)) return st;
     if (!cu_new || !aligned(cu_new, 4)) return STEM_ERR_INVALID_ARG;
     if (shape->tokens == 0) return STEM_OK;
     if (!path || !aligned(path, 4) || !slots || !aligned(slots, 4)) return STEM_ERR_INVALID_ARG;
     if (pages->num_pages == 0) return STEM_OK;
     if (!k_pages || !aligned(k_pages, 16) || !v_pages || !aligned(v_pages, 16)) return STEM_ERR_INVALID_ARG;
-    const int32_t bytes = dtype == STEM_FP32 ? 4 : 2;
     const CommitCall call = {*shape, *pages, num_kv_heads, head_dim * bytes, bytes, path, slots, cu_new, k_pages, v_pages};
     return launch_tree_commit(call, static_cast<hipStream_t>(hip_stream));
 }

@@ -129,7 +129,8 @@ class PagedCache:
         self.accepted, self.accept_status = whole(self.requests), whole(2)
         self.path = whole(max(self.tokens, 1), value=-1)
         self.next_ids = {t: torch.full((self.requests,), -1, dtype=t, device=device) for t in (torch.int32, torch.int64)}
-        self._step_open = False                            # whether there is a step of which nothing has been accepted yet
+        # whether there is a step of which nothing has been accepted yet; None once a step has been captured, as nobody here sees its replays
+        self._step_open: Optional[bool] = False
 
     def advance(self, new_lens: Optional[torch.Tensor] = None, max_new: int = 0) -> None:
         """Room for a step: new_lens int32 [requests] new tokens (None: one each; negative: the request has finished and its pages
@@ -137,7 +138,8 @@ class PagedCache:
         there is no room changes none of the first two, has no tokens and says so in status (see refused)."""
         self.shape.c.max_new = max_new
         self._offset_open = False
-        self._step_open = True
+        if self._step_open is not None:
+            self._step_open = None if self._capturing() else True
         db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
                             self.cu_new, self.positions, self.slots, self.status, self.workspace)
 
@@ -163,10 +165,12 @@ class PagedCache:
         """What is kept of the last step's new tokens, of which parents int32 [tokens] says behind which number of its request's new ones each
         was drafted: a request's first one, and behind a kept one the draft that is the model's own choice there.  draft_ids and target_ids
         (int32 or int64 [tokens]): the token in each row, and the model's choice behind it.  Brings lengths and free pages up to date and
-        moves the kept tokens' keys and values up; once per step.  Returns (accepted int32 [requests], path int32 [tokens], next_ids
+        moves the kept tokens' keys and values up; once per step (a second time raises, unless steps are replayed from a graph, where nobody
+        sees it).  Returns (accepted int32 [requests], path int32 [tokens], next_ids
         [requests]), as stem_tree_accept has them, in buffers of the cache.  What cannot be done changes nothing and shows in
         accept_refused."""
-        if not self._step_open:
+        capturing = self._capturing()                      # (of the step before a replay, whichever that will be)
+        if self._step_open is False and not capturing:
             raise RuntimeError("there is no step of which anything could be accepted")
         c, ids = self.shape.c, draft_ids.dtype
         if ids not in self.next_ids:
@@ -175,9 +179,13 @@ class PagedCache:
         shape = tb.AcceptShape(c.requests, self.tokens, max_new, c.page_size, c.num_pages, c.pages_per_request)
         tb.stem_tree_accept(shape, parents, draft_ids, target_ids, self.cu_new, self.lens, self.ring_state, self.ring, self.table, self.lens,
                             self.ring_state, self.accepted, self.path, self.next_ids[ids], self.accept_status, self.workspace)
-        self._step_open = False
+        if self._step_open and not capturing:
+            self._step_open = False
         tb.stem_tree_commit(shape, self.pages, self.path, self.slots, self.cu_new, self.k_pages, self.v_pages)
         return self.accepted, self.path, self.next_ids[ids]
+
+    def _capturing(self) -> bool:
+        return self.k_pages.is_cuda and torch.cuda.is_current_stream_capturing()
 
     def accept_refused(self) -> Tuple[int, int]:
         """Why the last accept was refused, if it was: requests with unusable numbers of tokens; room for pages given back.  Waits for the
