@@ -9,8 +9,10 @@
 // sums over a head are a few exchanges between neighbouring lanes, and the row is read once.  A wave takes 64 / lanes heads at a
 // time, a workgroup a few tokens, whose (cos, sin) it computes once, beside the weights, into LDS.
 //
-// Heads whose halves do not begin at 16 bytes, or that are longer than 64 lanes hold, go one wave each, a pair of values per lane at a
-// time, read twice (the second time from the caches).
+// Halves that do not both begin at 16 bytes lie in the lanes as they lie in memory, and are exchanged through LDS: what is lost is the
+// vector instructions for the places there (16384 tokens of 32 + 8 heads of 128, 50 values of each turning, bf16: 124 us, backwards 199; with
+// one pair of values per lane at a time, as below, 312 and 674; 48 values: 75 and 144).  Heads that are longer than 64 lanes hold (fp32 beyond
+// 512 values) go one wave each, a pair of values per lane at a time, read twice (the second time from the caches).
 #include "stem_rotary_common.h"
 #include "stem_norm_common.h"
 
@@ -36,6 +38,8 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 256;
+// How pairs lie in a lane's values: neighbours; the two chunks; or one of them in another lane.
+enum Pairs { kNeighbours, kHalves, kAcross };
 constexpr int kNormPairs = 2048;                       // (cos, sin) that a workgroup holds at most
 
 // v_rsq_f32 is within 1 ulp; its argument is a normal number, as eps is one
@@ -70,50 +74,85 @@ __device__ __forceinline__ void weights_to(float* w, const NormArgs& a) {
         w[a.head_dim + i] = weight_at(a.k_weight, a.weight_dtype, a.weight_offset, i);
     }
 }
+// Place of pair i's (cos, sin) among a token's where lanes 16 pairs apart read at a time: over all banks.
+__host__ __device__ __forceinline__ int spread(int i) { return i + (i >> 4); }
 // (cos, sin) of `here` tokens from t0 on -> [here][padded]; pairs behind the rotary part turn by nothing
+template <bool SPREAD>
 __device__ __forceinline__ void turns_to(float2* turn_of, const NormArgs& a, int t0, int here) {
-    for (int x = threadIdx.x; x < here * a.padded; x += kNormThreads) {
-        const int t = x / a.padded, i = x - t * a.padded;
+    const int pairs = SPREAD ? a.half : a.padded;
+    for (int x = threadIdx.x; x < here * pairs; x += kNormThreads) {
+        const int t = x / pairs, i = x - t * pairs;
         float2 cs = make_float2(1.f, 0.f);
         if (i < a.half) {
             cs = cos_sin((double)a.positions[t0 + t] * a.turns[i]);
             cs = make_float2(cs.x * a.factor, cs.y * a.sine_factor);
         }
-        turn_of[x] = cs;
+        turn_of[t * a.padded + (SPREAD ? spread(i) : i)] = cs;
     }
 }
 
 // What a lane has of a head: the values at `first` and `second`, W each.
 struct Item {
-    int first, second, pair;                           // pair: number of the first's first pair, -1 if the item does not turn
+    int first, second, pair;                           // pair: number of the first's first pair, -1 if the item does not turn (kAcross: 0 or -1)
     bool has_first, has_second;
 };
-template <typename T, bool HALF>
+template <typename T, Pairs PAIRS>
 __device__ __forceinline__ Item item_of(const NormArgs& a, int i) {
     constexpr int W = 16 / sizeof(T);
     Item it;
-    if (HALF && i < a.turning) {                       // chunk i of the one half and of the other
+    if (PAIRS == kHalves && i < a.turning) {           // chunk i of the one half and of the other
         it.first = i * W, it.second = a.half + i * W, it.pair = i * W;
     } else {
-        it.first = HALF ? 2 * a.half + (i - a.turning) * 2 * W : i * 2 * W;
+        it.first = PAIRS == kHalves ? 2 * a.half + (i - a.turning) * 2 * W : i * 2 * W;
         it.second = it.first + W;
-        it.pair = !HALF && i < a.turning ? i * W : -1;
+        it.pair = PAIRS == kHalves || i >= a.turning ? -1 : PAIRS == kNeighbours ? i * W : 0;
     }
     it.has_first = i < a.items && it.first < a.head_dim;
     it.has_second = i < a.items && it.second < a.head_dim;
     return it;
 }
 
-// n turned: pairs (x[e], x[W + e]) or neighbours
-template <int W, bool HALF>
-__device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs) {
+// A lane's values turned.  PAIRS says where the other of a pair is: in x[W + e], next to it, or in the lane that has the value
+// `half` further on or back.  cs: (cos, sin) of the item's first pair; kAcross: of the token's.
+// exchange: what the wave's lanes hand each other, [2 W values][64 lanes], so that one value of all lanes lies in different banks, wherever
+// its lane is.
+template <int W, Pairs PAIRS>
+__device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs, const Item& it, int half, float* exchange) {
+    if constexpr (PAIRS == kAcross) {
+        const int lane = threadIdx.x & 63;
+        int first = it.first;
+        asm("" : "+v"(first));                         // (places that are kept for the next head are registers that the loads need)
+        const int head_lane0 = lane - first / (2 * W);
 #pragma unroll
-    for (int e = 0; e < W; ++e) {
-        float &p = HALF ? x[e] : x[2 * e], &r = HALF ? x[W + e] : x[2 * e + 1];
-        const float2 c = cs[e];
-        const float y = p * c.x - r * c.y;
-        r = r * c.x + p * c.y;
-        p = y;
+        for (int e = 0; e < 2 * W; ++e) exchange[e * 64 + lane] = x[e];
+        // (all lanes of a head are in one wave, whose reads and writes of LDS stay in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        float2 c[2 * W];
+        float other[2 * W];
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e) {              // (all asked for before any is used)
+            const int i = first + e, pair = i < half ? i : i < 2 * half ? i - half : 0, j = i < half ? i + half : pair;
+            c[e] = cs[spread(pair)];
+            other[e] = exchange[j % (2 * W) * 64 + head_lane0 + j / (2 * W)];
+        }
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e) {
+            const int i = first + e;
+            const float y = x[e] * c[e].x + (i < half ? -other[e] : other[e]) * c[e].y;
+            x[e] = i < 2 * half ? y : x[e];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            float &p = PAIRS == kHalves ? x[e] : x[2 * e], &r = PAIRS == kHalves ? x[W + e] : x[2 * e + 1];
+            const float2 c = cs[e];
+            const float y = p * c.x - r * c.y;
+            r = r * c.x + p * c.y;
+            p = y;
+        }
     }
 }
 
@@ -168,18 +207,19 @@ __device__ __forceinline__ bool place_row(const NormArgs& a, int t0, uint32_t ro
     return true;
 }
 
-template <typename T, bool HALF, bool PAGES, bool STREAM>
+template <typename T, Pairs PAIRS, bool PAGES, bool STREAM>
 __global__ __launch_bounds__(kNormThreads) void norm_rotary_kernel(NormArgs a) {
     constexpr int W = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char norm_lds[];
     float* const weights = reinterpret_cast<float*>(norm_lds);
-    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim);
+    float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> 6) * 2 * W * 64;
+    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * W : 0));
     const int t0 = blockIdx.x * a.per_block, here = min(a.per_block, a.tokens - t0);
     weights_to(weights, a);
-    turns_to(turn_of, a, t0, here);
+    turns_to<PAIRS == kAcross>(turn_of, a, t0, here);
     __syncthreads();
     const int lane = threadIdx.x & ((1 << a.lane_bits) - 1);
-    const Item it = item_of<T, HALF>(a, lane);
+    const Item it = item_of<T, PAIRS>(a, lane);
     const uint32_t rows = (uint32_t)here * (a.Hq + (PAGES ? 2 : 1) * a.Hkv);
     for (uint32_t row = threadIdx.x >> a.lane_bits; row < rows; row += kNormThreads >> a.lane_bits) {
         const T* src;
@@ -194,7 +234,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_kernel(NormArgs a) {
             for (int e = 0; e < 2 * W; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
             const float r = inverse_root(__builtin_fmaf(head_sum(sum, a.lane_bits), a.by_dim, a.eps));
             scale_item<W>(x, weights + (kind == 0 ? 0 : a.head_dim), it, r);
-            if (it.pair >= 0) turn<W, HALF>(x, turn_of + t * a.padded + it.pair);
+            if (it.pair >= 0) turn<W, PAIRS>(x, turn_of + t * a.padded + it.pair, it, a.half, exchange);
         }
         store_item<T, W, STREAM>(dst, x, it);
     }
@@ -208,7 +248,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_any_kernel(NormArgs 
     float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim);
     const int t0 = blockIdx.x * a.per_block, here = min(a.per_block, a.tokens - t0);
     weights_to(weights, a);
-    turns_to(turn_of, a, t0, here);
+    turns_to<false>(turn_of, a, t0, here);
     __syncthreads();
     const int lane = threadIdx.x & 63;
     const uint32_t rows = (uint32_t)here * (a.Hq + (PAGES ? 2 : 1) * a.Hkv);
@@ -241,10 +281,10 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_any_kernel(NormArgs 
 }
 
 // One tensor's heads of `here` tokens: its gradients, and the lane's share of its weights' into acc.
-template <typename T, bool HALF, bool STREAM>
+template <typename T, Pairs PAIRS, bool STREAM>
 __device__ __forceinline__ void backward_rows(const NormArgs& a, const void* x_base, const void* g_base, void* out, int64_t st, int64_t sh,
                                               int64_t go_st, int64_t go_sh, int heads, FastDiv by, const float* w, const float2* turn_of,
-                                              int t0, int here, const Item& it, float (&acc)[2 * (16 / sizeof(T))]) {
+                                              float* exchange, int t0, int here, const Item& it, float (&acc)[2 * (16 / sizeof(T))]) {
     constexpr int W = 16 / sizeof(T);
     const uint32_t rows = (uint32_t)here * heads;
     for (uint32_t row = threadIdx.x >> a.lane_bits; row < rows; row += kNormThreads >> a.lane_bits) {
@@ -253,7 +293,7 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const void* x_b
         float x[2 * W], g[2 * W];
         load_item<T, W, STREAM>(x, static_cast<const T*>(x_base) + token * st + h * sh, it);
         load_item<T, W, STREAM>(g, static_cast<const T*>(g_base) + token * go_st + h * go_sh, it);
-        if (it.pair >= 0) turn<W, HALF>(g, turn_of + t * a.padded + it.pair);
+        if (it.pair >= 0) turn<W, PAIRS>(g, turn_of + t * a.padded + it.pair, it, a.half, exchange);
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 2 * W; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
@@ -275,27 +315,28 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const void* x_b
 }
 
 // A workgroup has per_block tokens, per_step at a time.
-template <typename T, bool HALF, bool STREAM>
+template <typename T, Pairs PAIRS, bool STREAM>
 __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormArgs a) {
     constexpr int W = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char norm_lds[];
     float* const weights = reinterpret_cast<float*>(norm_lds);
-    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim);
+    float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> 6) * 2 * W * 64;
+    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * W : 0));
     const int first = blockIdx.x * a.per_block, end = min(first + a.per_block, a.tokens);
     const int lane = threadIdx.x & ((1 << a.lane_bits) - 1);
-    const Item it = item_of<T, HALF>(a, lane);
+    const Item it = item_of<T, PAIRS>(a, lane);
     float acc_q[2 * W] = {}, acc_k[2 * W] = {};
     weights_to(weights, a);
     for (int t0 = first; t0 < end; t0 += a.per_step) {
         const int here = min(a.per_step, end - t0);
-        turns_to(turn_of, a, t0, here);
+        turns_to<PAIRS == kAcross>(turn_of, a, t0, here);
         __syncthreads();
         if (a.Hq > 0)
-            backward_rows<T, HALF, STREAM>(a, a.q, a.gq, a.q_out, a.q_st, a.q_sh, a.qo_st, a.qo_sh, a.Hq, a.by_q, weights, turn_of, t0, here,
-                                           it, acc_q);
+            backward_rows<T, PAIRS, STREAM>(a, a.q, a.gq, a.q_out, a.q_st, a.q_sh, a.qo_st, a.qo_sh, a.Hq, a.by_q, weights, turn_of, exchange,
+                                            t0, here, it, acc_q);
         if (a.Hkv > 0)
-            backward_rows<T, HALF, STREAM>(a, a.k, a.gk, a.k_out, a.k_st, a.k_sh, a.ko_st, a.ko_sh, a.Hkv, a.by_k, weights + a.head_dim,
-                                           turn_of, t0, here, it, acc_k);
+            backward_rows<T, PAIRS, STREAM>(a, a.k, a.gk, a.k_out, a.k_st, a.k_sh, a.ko_st, a.ko_sh, a.Hkv, a.by_k, weights + a.head_dim,
+                                            turn_of, exchange, t0, here, it, acc_k);
         __syncthreads();
     }
     if (!a.partial) return;
@@ -334,7 +375,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_any_kernel(NormArg
     for (int i = threadIdx.x; i < kWaves * 2 * a.head_dim; i += kNormThreads) sums[i] = 0.f;
     for (int t0 = first; t0 < end; t0 += a.per_step) {
         const int here = min(a.per_step, end - t0);
-        turns_to(turn_of, a, t0, here);
+        turns_to<false>(turn_of, a, t0, here);
         __syncthreads();
         const uint32_t rows = (uint32_t)here * (a.Hq + a.Hkv);
         for (uint32_t row = wave; row < rows; row += kWaves) {
@@ -421,8 +462,8 @@ __global__ __launch_bounds__(kColumns * kSumRows) void norm_weights_kernel(const
     if (out) out[i < head_dim ? i : i - head_dim] = (float)sum;
 }
 
-// A launch's arguments but for its split into workgroups; whether heads lie in registers.
-static bool arguments_of(const NormCall& c, NormArgs& a) {
+// A launch's arguments but for its split into workgroups; whether heads lie in registers, and how.
+static bool arguments_of(const NormCall& c, NormArgs& a, Pairs& pairs) {
     const RotaryCall& r = c.rotary;
     const stem_rotary_shape& s = r.shape;
     const bool pages = r.slots != nullptr, half_layout = s.layout == STEM_ROTARY_HALF;
@@ -436,10 +477,11 @@ static bool arguments_of(const NormCall& c, NormArgs& a) {
     a.factor = r.factor, a.sine_factor = r.backward ? -r.factor : r.factor;
     a.eps = c.norm.eps, a.weight_offset = c.norm.weight_offset, a.by_dim = 1.f / s.head_dim, a.weight_dtype = c.norm.weight_dtype;
     a.tokens = s.tokens, a.Hq = s.num_q_heads, a.Hkv = s.num_kv_heads, a.half = s.rotary_dim / 2, a.head_dim = s.head_dim;
-    a.turning = half_layout ? a.half / W : (s.rotary_dim + 2 * W - 1) / (2 * W);
-    a.items = half_layout ? a.turning + (s.head_dim - s.rotary_dim + 2 * W - 1) / (2 * W) : (s.head_dim + 2 * W - 1) / (2 * W);
-    const bool wide = (!half_layout || a.half % W == 0) && a.items <= 64;
-    a.padded = wide ? a.turning * W : a.half;
+    pairs = !half_layout ? kNeighbours : a.half % W == 0 ? kHalves : kAcross;
+    a.turning = (s.rotary_dim + 2 * W - 1) / (2 * W);  // (kHalves: whole chunks of either half)
+    a.items = (s.head_dim + 2 * W - 1) / (2 * W);
+    const bool wide = a.items <= 64;
+    a.padded = !wide ? a.half : pairs == kAcross ? spread(a.half - 1) + 1 : a.turning * W;
     a.lane_bits = 2;
     while (1 << a.lane_bits < a.items && a.lane_bits < 6) ++a.lane_bits;
     if (!wide) a.lane_bits = 6;
@@ -466,24 +508,32 @@ static int tokens_for(const NormArgs& a, int heads) {
     return n < 1 ? 1 : n;
 }
 
+// LDS of the weights, of what lanes exchange, and of the (cos, sin) of per_step tokens
 template <typename T>
-static void launch_forward(const NormArgs& a, bool wide, bool half_layout, bool pages, bool through, hipStream_t stream) {
+static size_t lds_of(const NormArgs& a, bool exchanges) {
+    return sizeof(float) * (2 * a.head_dim + (exchanges ? kNormThreads * 2 * (16 / sizeof(T)) : 0)) + sizeof(float2) * (size_t)a.per_step * a.padded;
+}
+
+template <typename T>
+static void launch_forward(const NormArgs& a, bool wide, Pairs pairs, bool pages, bool through, hipStream_t stream) {
     const dim3 grid((a.tokens + a.per_block - 1) / a.per_block), block(kNormThreads);
-    const size_t lds = 2 * sizeof(float) * a.head_dim + sizeof(float2) * (size_t)a.per_block * a.padded;
+    const size_t lds = lds_of<T>(a, wide && pairs == kAcross);
     if (!wide) {
+        const bool half_layout = pairs != kNeighbours;
         if (pages) hipLaunchKernelGGL((norm_rotary_any_kernel<T, true>), grid, block, lds, stream, a, half_layout);
         else hipLaunchKernelGGL((norm_rotary_any_kernel<T, false>), grid, block, lds, stream, a, half_layout);
         return;
     }
-#define STEM_NORM_LAUNCH(HALF, PAGES)                                                                                    \
+#define STEM_NORM_LAUNCH(PAIRS)                                                                                          \
     do {                                                                                                                 \
-        if (through) hipLaunchKernelGGL((norm_rotary_kernel<T, HALF, PAGES, true>), grid, block, lds, stream, a);        \
-        else hipLaunchKernelGGL((norm_rotary_kernel<T, HALF, PAGES, false>), grid, block, lds, stream, a);               \
+        if (pages && through) hipLaunchKernelGGL((norm_rotary_kernel<T, PAIRS, true, true>), grid, block, lds, stream, a);   \
+        else if (pages) hipLaunchKernelGGL((norm_rotary_kernel<T, PAIRS, true, false>), grid, block, lds, stream, a);    \
+        else if (through) hipLaunchKernelGGL((norm_rotary_kernel<T, PAIRS, false, true>), grid, block, lds, stream, a);  \
+        else hipLaunchKernelGGL((norm_rotary_kernel<T, PAIRS, false, false>), grid, block, lds, stream, a);              \
     } while (0)
-    if (half_layout && pages) STEM_NORM_LAUNCH(true, true);
-    else if (half_layout) STEM_NORM_LAUNCH(true, false);
-    else if (pages) STEM_NORM_LAUNCH(false, true);
-    else STEM_NORM_LAUNCH(false, false);
+    if (pairs == kHalves) STEM_NORM_LAUNCH(kHalves);
+    else if (pairs == kNeighbours) STEM_NORM_LAUNCH(kNeighbours);
+    else STEM_NORM_LAUNCH(kAcross);
 #undef STEM_NORM_LAUNCH
 }
 
@@ -492,39 +542,43 @@ static size_t value_bytes(int32_t dtype) { return dtype == STEM_FP32 ? 4 : 2; }
 int launch_norm_rotary(const NormCall& c, hipStream_t stream) {
     const stem_rotary_shape& s = c.rotary.shape;
     NormArgs a;
-    const bool wide = arguments_of(c, a), pages = c.rotary.slots != nullptr, half_layout = s.layout == STEM_ROTARY_HALF;
+    Pairs pairs;
+    const bool wide = arguments_of(c, a, pairs), pages = c.rotary.slots != nullptr;
     const int heads = a.Hq + (pages ? 2 : 1) * a.Hkv;
     a.per_block = a.per_step = tokens_for(a, heads);
     const bool through = (int64_t)s.tokens * heads * s.head_dim * value_bytes(s.dtype) > 64 << 20;
-    if (s.dtype == STEM_BF16) launch_forward<__bf16>(a, wide, half_layout, pages, through, stream);
-    else if (s.dtype == STEM_FP16) launch_forward<_Float16>(a, wide, half_layout, pages, through, stream);
-    else launch_forward<float>(a, wide, half_layout, pages, through, stream);
+    if (s.dtype == STEM_BF16) launch_forward<__bf16>(a, wide, pairs, pages, through, stream);
+    else if (s.dtype == STEM_FP16) launch_forward<_Float16>(a, wide, pairs, pages, through, stream);
+    else launch_forward<float>(a, wide, pairs, pages, through, stream);
     return check_launch();
 }
 
 template <typename T>
-static void launch_backward(const NormArgs& a, bool wide, bool half_layout, bool through, hipStream_t stream) {
+static void launch_backward(const NormArgs& a, bool wide, Pairs pairs, bool through, hipStream_t stream) {
     const dim3 grid((a.tokens + a.per_block - 1) / a.per_block), block(kNormThreads);
-    const size_t turns = sizeof(float2) * (size_t)a.per_step * a.padded, weights = 2 * sizeof(float) * a.head_dim;
     if (!wide) {
-        hipLaunchKernelGGL((norm_backward_any_kernel<T>), grid, block, weights * (1 + kNormThreads / 64) + turns, stream, a, half_layout);
+        const size_t lds = lds_of<T>(a, false) + 2 * sizeof(float) * a.head_dim * (kNormThreads / 64);
+        hipLaunchKernelGGL((norm_backward_any_kernel<T>), grid, block, lds, stream, a, pairs != kNeighbours);
         return;
     }
-    const size_t sums = sizeof(float) * (size_t)(kNormThreads >> a.lane_bits) * a.head_dim, lds = weights + turns > sums ? weights + turns : sums;
-#define STEM_NORM_LAUNCH(HALF)                                                                                           \
+    const size_t sums = sizeof(float) * (size_t)(kNormThreads >> a.lane_bits) * a.head_dim, others = lds_of<T>(a, pairs == kAcross);
+    const size_t lds = others > sums ? others : sums;
+#define STEM_NORM_LAUNCH(PAIRS)                                                                                          \
     do {                                                                                                                 \
-        if (through) hipLaunchKernelGGL((norm_backward_kernel<T, HALF, true>), grid, block, lds, stream, a);             \
-        else hipLaunchKernelGGL((norm_backward_kernel<T, HALF, false>), grid, block, lds, stream, a);                    \
+        if (through) hipLaunchKernelGGL((norm_backward_kernel<T, PAIRS, true>), grid, block, lds, stream, a);            \
+        else hipLaunchKernelGGL((norm_backward_kernel<T, PAIRS, false>), grid, block, lds, stream, a);                   \
     } while (0)
-    if (half_layout) STEM_NORM_LAUNCH(true);
-    else STEM_NORM_LAUNCH(false);
+    if (pairs == kHalves) STEM_NORM_LAUNCH(kHalves);
+    else if (pairs == kNeighbours) STEM_NORM_LAUNCH(kNeighbours);
+    else STEM_NORM_LAUNCH(kAcross);
 #undef STEM_NORM_LAUNCH
 }
 
 int launch_norm_rotary_backward(const NormCall& c, hipStream_t stream) {
     const stem_rotary_shape& s = c.rotary.shape;
     NormArgs a;
-    const bool wide = arguments_of(c, a), half_layout = s.layout == STEM_ROTARY_HALF;
+    Pairs pairs;
+    const bool wide = arguments_of(c, a, pairs);
     const int parts = norm_parts(s.tokens);
     if (parts > 0) {
         a.per_block = (s.tokens + parts - 1) / parts;
@@ -532,9 +586,9 @@ int launch_norm_rotary_backward(const NormCall& c, hipStream_t stream) {
         a.per_step = tokens_for(a, fewest);
         if (a.per_step > a.per_block) a.per_step = a.per_block;
         const bool through = (int64_t)s.tokens * (a.Hq + a.Hkv) * s.head_dim * value_bytes(s.dtype) > 64 << 20;
-        if (s.dtype == STEM_BF16) launch_backward<__bf16>(a, wide, half_layout, through, stream);
-        else if (s.dtype == STEM_FP16) launch_backward<_Float16>(a, wide, half_layout, through, stream);
-        else launch_backward<float>(a, wide, half_layout, through, stream);
+        if (s.dtype == STEM_BF16) launch_backward<__bf16>(a, wide, pairs, through, stream);
+        else if (s.dtype == STEM_FP16) launch_backward<_Float16>(a, wide, pairs, through, stream);
+        else launch_backward<float>(a, wide, pairs, through, stream);
         if (const int st = check_launch()) return st;
         if (!a.partial) return STEM_OK;
     }
