@@ -1,4 +1,4 @@
-"""Builds libstem_hip.so (the C-ABI library) for gfx950 with hipcc, in-tree.
+"""Builds libstem_hip.so (the C-ABI library) for gfx950 with hipcc, and the module that checks tensors for its bindings, in-tree.
 
 Run as `python -m paper_2603_06274_amd.build`.  Cross-compiles without a GPU.
 """
@@ -15,6 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libstem_hip.so")
+TENSORS = os.path.join(PKG, "_tensors.so")               # the bindings' checks of tensors, for this Python and this torch
 
 SOURCES = ["stem_api.cpp", "stem_pool.hip", "stem_scores.hip", "stem_select.hip", "stem_attn.hip", "stem_static.hip",
            "stem_decode_api.cpp", "stem_rotary.hip", "stem_table.hip", "stem_prefix.hip", "stem_norm_api.cpp", "stem_norm.hip",
@@ -57,6 +58,22 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
+def build_tensors() -> None:
+    """The Python module of csrc/tensors_module.cpp: host code alone, against torch's headers and libraries."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    includes = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
+    cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(), *("-isystem" + x for x in includes),
+           os.path.join(CSRC, "tensors_module.cpp"), "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", TENSORS]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("tensors_module.cpp does not build:\n%s\n%s" % (res.stdout, res.stderr))
+
+
 def check_wait_states(extra=()) -> None:
     """The attention kernel places some matrix instructions (and the wait states they need) by hand:
     compile it to assembly once more and verify the distances in what the compiler made of it."""
@@ -80,10 +97,10 @@ def check_wait_states(extra=()) -> None:
 
 def build(extra_flags=(), verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as ex:
-        checked = ex.submit(check_wait_states, list(extra_flags))
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 2)) as ex:
+        checked, tensors = ex.submit(check_wait_states, list(extra_flags)), ex.submit(build_tensors)
         objs = list(ex.map(lambda s: _compile(s, list(extra_flags)), SOURCES))
-        checked.result()
+        checked.result(), tensors.result()
     cmd = [hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", LIB]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

@@ -152,6 +152,15 @@ def _lines(t: Optional[torch.Tensor], n: int, each: int, name: str, dev: int, dt
     return t.data_ptr()
 
 
+try:                                                   # the same three in compiled code, for tensors that are as they have to be
+    from . import _tensors
+except ImportError:                                    # (not built)
+    _tensors = None
+else:
+    _tensors.begin(_values, _whole, _lines)
+    _values, _whole, _lines = _tensors.values, _tensors.whole, _tensors.lines
+
+
 def _seen(t: Optional[torch.Tensor]) -> Optional[tuple]:
     return None if t is None else (t.shape, t.stride(), t.dtype)
 
