@@ -75,12 +75,10 @@ __device__ __forceinline__ bool bad_request(const AcceptCall& a, int len, int n)
     return n > a.shape.max_new || len < n || len > (int64_t)a.shape.pages_per_request * a.shape.page_size;
 }
 
-// One wave per request.  A token that is its parent's choice offers itself to the parent, of several the lowest-numbered; then the kept ones are
-// a walk along these offers.
+// One wave's walk of request r.  A token that is its parent's choice offers itself to the parent, of several the lowest-numbered; then the kept
+// ones are a walk along these offers.  lds: [max_new] offers, [max_new] path, [max_new] choices.
 template <typename Id>
-__global__ __launch_bounds__(64) void tree_walk_kernel(AcceptCall a) {
-    extern __shared__ int32_t walk_lds[];              // [max_new] offers, [max_new] path, [max_new] choices
-    const int r = blockIdx.x, lane = threadIdx.x;
+__device__ __forceinline__ void walk_request(const AcceptCall& a, int r, int lane, int32_t* lds) {
     int first, n;
     tree_tokens(a.cu_new, a.shape.tokens, r, first, n);
     Id* const next = static_cast<Id*>(a.next_ids);
@@ -92,19 +90,24 @@ __global__ __launch_bounds__(64) void tree_walk_kernel(AcceptCall a) {
         return;
     }
     const int most = a.shape.max_new;
-    int32_t *const offer = walk_lds, *const kept = walk_lds + most;
-    Id* const choice = reinterpret_cast<Id*>(walk_lds + 2 * most);
+    int32_t *const offer = lds, *const kept = lds + most;
+    Id* const choice = reinterpret_cast<Id*>(lds + 2 * most);
     constexpr int kNone = 0x7fffffff;
+    // (a wave's reads and writes of LDS stay in order: the compiler has to keep them so)
+    auto in_order = [] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
     for (int i = lane; i < n; i += 64) {
         offer[i] = kNone;
         choice[i] = targets[i];
     }
-    __syncthreads();
+    in_order();
     for (int i = lane; i < n; i += 64) {
         const int p = a.parents[first + i];
         if (p >= 0 && p < i && drafts[i] == choice[p]) atomicMin(&offer[p], i);
     }
-    __syncthreads();
+    in_order();
     int count = 0, here = 0, last = 0;                 // the same in all lanes
     while (here != kNone) {
         if (lane == 0) kept[count] = here;
@@ -112,15 +115,28 @@ __global__ __launch_bounds__(64) void tree_walk_kernel(AcceptCall a) {
         last = here;
         here = offer[here];
     }
-    __syncthreads();
+    in_order();
     for (int i = lane; i < n; i += 64) path[i] = i < count ? kept[i] : -1;
     if (lane == 0) a.accepted[r] = count, next[r] = choice[last];
 }
+template <typename Id>
+__global__ __launch_bounds__(64) void tree_walk_kernel(AcceptCall a) {
+    extern __shared__ int32_t walk_lds[];
+    walk_request<Id>(a, blockIdx.x, threadIdx.x, walk_lds);
+}
 
 // One workgroup: lengths without the tokens that are not kept, and the pages behind them back to the ring, which takes sums over the requests.
+// WALKS: of few requests it does the walks as well, a wave each.
 constexpr int kBooksThreads = 1024;
-template <typename Id>
+template <typename Id, bool WALKS>
 __global__ __launch_bounds__(kBooksThreads) void tree_books_kernel(AcceptCall a) {
+    extern __shared__ int32_t walks_lds[];             // WALKS: [waves] as a walk has it
+    if constexpr (WALKS) {
+        const int w = threadIdx.x >> 6;                // as many waves as requests
+        int32_t* const mine = walks_lds + w * a.shape.max_new * (2 + (int)sizeof(Id) / 4);
+        walk_request<Id>(a, w, threadIdx.x & 63, mine);
+        __syncthreads();
+    }
     __shared__ int2 wave_sums[kBooksThreads / 64];     // pages back, bad requests
     const int tid = threadIdx.x, w = tid >> 6, waves = blockDim.x >> 6;
     const int shift = __builtin_ctz(a.shape.page_size), mask = a.shape.page_size - 1, pages = a.shape.num_pages;
@@ -193,16 +209,27 @@ __global__ __launch_bounds__(kBooksThreads) void tree_books_kernel(AcceptCall a)
     }
 }
 
-int launch_tree_accept(const AcceptCall& c, hipStream_t stream) {
+// Up to 16 requests in one launch (16 drafts each, 16 requests: 5.1 us a call and 5.0 in a graph, with two launches 8.0 and 5.5; 256 drafts 6.4 and
+// 6.5, 8.3 and 6.8).  Two walks after the other in a wave are slower in a graph: 32 requests 6.1 and 5.6.
+constexpr int kWalksAtOnce = kBooksThreads / 64;
+constexpr size_t kWalksLds = 64 << 10;
+
+template <typename Id>
+static int launch_accept(const AcceptCall& c, hipStream_t stream) {
     const stem_accept_shape& s = c.shape;
+    const size_t lds = (size_t)s.max_new * (2 * sizeof(int32_t) + sizeof(Id));
+    if (s.requests <= kWalksAtOnce && s.requests * lds <= kWalksLds) {
+        hipLaunchKernelGGL((tree_books_kernel<Id, true>), dim3(1), dim3(s.requests * 64), s.requests * lds, stream, c);
+        return check_launch();
+    }
     const dim3 lanes(s.requests < kBooksThreads ? (s.requests + 63) / 64 * 64 : kBooksThreads);
-    const size_t lds = (size_t)s.max_new * (2 * sizeof(int32_t) + s.id_bits / 8);
-    if (s.id_bits == 32) hipLaunchKernelGGL(tree_walk_kernel<int32_t>, dim3(s.requests), dim3(64), lds, stream, c);
-    else hipLaunchKernelGGL(tree_walk_kernel<int64_t>, dim3(s.requests), dim3(64), lds, stream, c);
+    hipLaunchKernelGGL(tree_walk_kernel<Id>, dim3(s.requests), dim3(64), lds, stream, c);
     if (const int st = check_launch()) return st;
-    if (s.id_bits == 32) hipLaunchKernelGGL(tree_books_kernel<int32_t>, dim3(1), lanes, 0, stream, c);
-    else hipLaunchKernelGGL(tree_books_kernel<int64_t>, dim3(1), lanes, 0, stream, c);
+    hipLaunchKernelGGL((tree_books_kernel<Id, false>), dim3(1), lanes, 0, stream, c);
     return check_launch();
+}
+int launch_tree_accept(const AcceptCall& c, hipStream_t stream) {
+    return c.shape.id_bits == 32 ? launch_accept<int32_t>(c, stream) : launch_accept<int64_t>(c, stream);
 }
 
 // --- kept rows move up --------------------------------------------------------------------------------------

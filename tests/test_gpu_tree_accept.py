@@ -68,7 +68,8 @@ class Books:
 @pytest.mark.parametrize("ids", [torch.int32, torch.int64])
 @pytest.mark.parametrize("requests,most_new,most_past,P,branch", [
     (1, 1, 5, 16, 1), (1, 40, 0, 16, 3), (7, 9, 100, 16, 1), (64, 16, 300, 64, 4), (64, 64, 300, 16, 2), (65, 65, 30, 32, 9),
-    (3, 1024, 50, 16, 1), (3, 1000, 50, 256, 500), (1500, 6, 40, 16, 2)])
+    (3, 1024, 50, 16, 1), (3, 1000, 50, 256, 500), (1500, 6, 40, 16, 2),
+    (16, 30, 100, 16, 3), (17, 30, 100, 16, 3), (16, 256, 100, 16, 2), (16, 257, 100, 16, 2), (6, 900, 100, 32, 4)])
 def test_matches_its_definition(ids, requests, most_new, most_past, P, branch):
     for seed in range(3):
         rng = random.Random(seed * 100 + requests)
