@@ -12,7 +12,7 @@ static int check_norm(const stem_head_norm* n) {
     return STEM_OK;
 }
 
-static size_t partial_bytes(const stem_rotary_shape& s) { return align256(2 * sizeof(float) * (size_t)norm_parts(s.tokens) * s.head_dim); }
+static size_t partial_bytes(const stem_rotary_shape& s) { return align256(2 * sizeof(float) * (size_t)norm_parts(s) * s.head_dim); }
 
 }  // namespace stem
 
