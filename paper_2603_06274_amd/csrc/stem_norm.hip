@@ -9,10 +9,10 @@
 // sums over a head are a few exchanges between neighbouring lanes, and the row is read once.  A wave takes 64 / lanes heads at a
 // time, a workgroup a few tokens, whose (cos, sin) it computes once, beside the weights, into LDS.
 //
-// Halves that do not both begin at 16 bytes lie in the lanes as they lie in memory, and are exchanged through LDS: what is lost is the
-// vector instructions for the places there (16384 tokens of 32 + 8 heads of 128, 50 values of each turning, bf16: 124 us, backwards 199; with
-// one pair of values per lane at a time, as below, 312 and 674; 48 values: 75 and 144).  Heads that are longer than 64 lanes hold (fp32 beyond
-// 512 values) go one wave each, a pair of values per lane at a time, read twice (the second time from the caches).
+// Halves that do not both begin at 16 bytes lie in the lanes as they lie in memory, and are exchanged through LDS: 16-bit values are bound by
+// that and its places (16384 tokens of 32 + 8 heads of 128, 50 values of each turning, bf16: 105 us, backwards 173; 48 values: 74 and 124;
+// fp32 values: 110 and 178, as fast as memory; one pair of values per lane at a time, as below: 312 and 674 in bf16).  Heads that are longer
+// than 64 lanes hold (fp32 beyond 512 values) go one wave each, a pair of values per lane at a time, read twice (the second time from the caches).
 #include "stem_rotary_common.h"
 #include "stem_norm_common.h"
 
@@ -29,7 +29,7 @@ struct NormArgs {
     int32_t weight_dtype;
     int32_t tokens, Hq, Hkv, half, padded, head_dim;   // half: pairs of a head; padded: with those that turn by nothing in LDS
     int32_t per_step, per_block;                       // tokens at a time, tokens of a workgroup
-    int32_t lane_bits, turning, items;                 // lanes of a head; items that turn; all (an item is two chunks)
+    int32_t lane_bits, turning, items;                 // lanes of a head; items of kHalves that turn; all items (of two chunks)
     FastDiv by_heads, by_q, by_k;
     int64_t q_st, q_sh, k_st, k_sh, qo_st, qo_sh, ko_st, ko_sh;
     int64_t page_st;                                   // k_out and v_out are pages: ko_st and ko_sh within one
@@ -74,10 +74,9 @@ __device__ __forceinline__ void weights_to(float* w, const NormArgs& a) {
         w[a.head_dim + i] = weight_at(a.k_weight, a.weight_dtype, a.weight_offset, i);
     }
 }
-// Place of pair i's (cos, sin) among a token's where lanes 16 pairs apart read at a time: over all banks.
-__host__ __device__ __forceinline__ int spread(int i) { return i + (i >> 4); }
-// (cos, sin) of `here` tokens from t0 on -> [here][padded]; pairs behind the rotary part turn by nothing
-template <bool SPREAD>
+// (cos, sin) of `here` tokens from t0 on -> [here][padded]; pairs behind the rotary part turn by nothing.  SPREAD > 0: with one place free
+// behind every SPREAD pairs.
+template <int SPREAD>
 __device__ __forceinline__ void turns_to(float2* turn_of, const NormArgs& a, int t0, int here) {
     const int pairs = SPREAD ? a.half : a.padded;
     for (int x = threadIdx.x; x < here * pairs; x += kNormThreads) {
@@ -87,44 +86,69 @@ __device__ __forceinline__ void turns_to(float2* turn_of, const NormArgs& a, int
             cs = cos_sin((double)a.positions[t0 + t] * a.turns[i]);
             cs = make_float2(cs.x * a.factor, cs.y * a.sine_factor);
         }
-        turn_of[t * a.padded + (SPREAD ? spread(i) : i)] = cs;
+        turn_of[t * a.padded + i + (SPREAD ? i / (SPREAD ? SPREAD : 1) : 0)] = cs;
     }
 }
 
-// What a lane has of a head: the values at `first` and `second`, W each.
+// What a lane has of a head: the chunks at `first` and `second`, W values each.  Neighbouring lanes have neighbouring chunks, so that a load or a
+// store of a wave is of whole lines (40961 tokens of 28 + 4 heads of 128, fp16, 64 values of each turning in neighbouring pairs: 118 us;
+// with 32 bytes in a row for a lane 157).
 struct Item {
-    int first, second, pair;                           // pair: number of the first's first pair, -1 if the item does not turn (kAcross: 0 or -1)
+    int first, second, pair, second_pair;              // the chunks' first pairs, -1 if a chunk does not turn (kHalves: one for both)
     bool has_first, has_second;
 };
 template <typename T, Pairs PAIRS>
 __device__ __forceinline__ Item item_of(const NormArgs& a, int i) {
     constexpr int W = 16 / sizeof(T);
     Item it;
-    if (PAIRS == kHalves && i < a.turning) {           // chunk i of the one half and of the other
-        it.first = i * W, it.second = a.half + i * W, it.pair = i * W;
+    if (PAIRS == kHalves) {                            // chunk i of the one half and of the other; behind them the others' two halves
+        const int rest = a.items - a.turning, x = i - a.turning;
+        it.first = i < a.turning ? i * W : 2 * a.half + x * W;
+        it.second = i < a.turning ? a.half + i * W : 2 * a.half + (rest + x) * W;
+        it.pair = it.second_pair = i < a.turning ? i * W : -1;
     } else {
-        it.first = PAIRS == kHalves ? 2 * a.half + (i - a.turning) * 2 * W : i * 2 * W;
-        it.second = it.first + W;
-        it.pair = PAIRS == kHalves || i >= a.turning ? -1 : PAIRS == kNeighbours ? i * W : 0;
+        it.first = i * W, it.second = (a.items + i) * W;
+        it.pair = it.first < 2 * a.half ? it.first / 2 : -1;
+        it.second_pair = it.second < 2 * a.half ? it.second / 2 : -1;
     }
     it.has_first = i < a.items && it.first < a.head_dim;
     it.has_second = i < a.items && it.second < a.head_dim;
     return it;
 }
 
-// A lane's values turned.  PAIRS says where the other of a pair is: in x[W + e], next to it, or in the lane that has the value
-// `half` further on or back.  cs: (cos, sin) of the item's first pair; kAcross: of the token's.
-// exchange: what the wave's lanes hand each other, [2 W values][64 lanes], so that one value of all lanes lies in different banks, wherever
-// its lane is.
+// A lane's values turned, if any of them turn.  PAIRS says where the other of a pair is: in x[W + e], next to it, or in the lane that has the value
+// `half` further on or back.  cs: a token's (cos, sin).
+// exchange: the head's values for its other lanes, W + 1 places to a chunk (as in cs), so that one value of all lanes lies in different
+// banks.  Values that do not turn ask for what lies there, and do not use it.
 template <int W, Pairs PAIRS>
-__device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs, const Item& it, int half, float* exchange) {
-    if constexpr (PAIRS == kAcross) {
-        const int lane = threadIdx.x & 63;
-        int first = it.first;
-        asm("" : "+v"(first));                         // (places that are kept for the next head are registers that the loads need)
-        const int head_lane0 = lane - first / (2 * W);
+__device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs, const Item& it, const NormArgs& a, float* exchange) {
+    if (it.pair < 0) return;
+    if constexpr (PAIRS == kHalves) {
 #pragma unroll
-        for (int e = 0; e < 2 * W; ++e) exchange[e * 64 + lane] = x[e];
+        for (int e = 0; e < W; ++e) {
+            const float2 c = cs[it.pair + e];
+            const float y = x[e] * c.x - x[W + e] * c.y;
+            x[W + e] = x[W + e] * c.x + x[e] * c.y;
+            x[e] = y;
+        }
+    } else if constexpr (PAIRS == kNeighbours) {
+        auto chunk = [&](float* v, const float2* c) {
+#pragma unroll
+            for (int e = 0; e < W / 2; ++e) {
+                const float y = v[2 * e] * c[e].x - v[2 * e + 1] * c[e].y;
+                v[2 * e + 1] = v[2 * e + 1] * c[e].x + v[2 * e] * c[e].y;
+                v[2 * e] = y;
+            }
+        };
+        chunk(x, cs + it.pair);
+        if (it.second_pair >= 0) chunk(x + W, cs + it.second_pair);
+    } else {
+        constexpr int S = W + 1;
+        const int half = a.half, shift = half / W, odd = half % W;
+        float* const mine[2] = {exchange + it.first / W * S, exchange + it.second / W * S};
+        const float2* const turn_at[2] = {cs + it.first / W * S, cs + it.second / W * S};
+#pragma unroll
+        for (int e = 0; e < 2 * W; ++e) mine[e / W][e % W] = x[e];
         // (all lanes of a head are in one wave, whose reads and writes of LDS stay in order)
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -132,27 +156,20 @@ __device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs, const 
         float other[2 * W];
 #pragma unroll
         for (int e = 0; e < 2 * W; ++e) {              // (all asked for before any is used)
-            const int i = first + e, pair = i < half ? i : i < 2 * half ? i - half : 0, j = i < half ? i + half : pair;
-            c[e] = cs[spread(pair)];
-            other[e] = exchange[j % (2 * W) * 64 + head_lane0 + j / (2 * W)];
+            // `half` values further on and back, from the chunk's begin: the same for all lanes
+            const int y = e % W, on = shift * S + y + odd + (y + odd >= W), back = y - shift * S - odd - (y < odd);
+            const bool in_first = (e < W ? it.first : it.second) + y < half;
+            other[e] = mine[e / W][in_first ? on : back];
+            c[e] = turn_at[e / W][in_first ? y : back];
         }
 #pragma unroll
         for (int e = 0; e < 2 * W; ++e) {
-            const int i = first + e;
+            const int i = (e < W ? it.first : it.second) + e % W;
             const float y = x[e] * c[e].x + (i < half ? -other[e] : other[e]) * c[e].y;
             x[e] = i < 2 * half ? y : x[e];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-    } else {
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            float &p = PAIRS == kHalves ? x[e] : x[2 * e], &r = PAIRS == kHalves ? x[W + e] : x[2 * e + 1];
-            const float2 c = cs[e];
-            const float y = p * c.x - r * c.y;
-            r = r * c.x + p * c.y;
-            p = y;
-        }
     }
 }
 
@@ -212,11 +229,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_kernel(NormArgs a) {
     constexpr int W = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char norm_lds[];
     float* const weights = reinterpret_cast<float*>(norm_lds);
-    float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> 6) * 2 * W * 64;
-    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * W : 0));
+    float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> a.lane_bits << a.lane_bits) * 2 * (W + 1);
+    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * (W + 1) : 0));
     const int t0 = blockIdx.x * a.per_block, here = min(a.per_block, a.tokens - t0);
     weights_to(weights, a);
-    turns_to<PAIRS == kAcross>(turn_of, a, t0, here);
+    turns_to<PAIRS == kAcross ? W : 0>(turn_of, a, t0, here);
     __syncthreads();
     const int lane = threadIdx.x & ((1 << a.lane_bits) - 1);
     const Item it = item_of<T, PAIRS>(a, lane);
@@ -234,7 +251,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_kernel(NormArgs a) {
             for (int e = 0; e < 2 * W; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
             const float r = inverse_root(__builtin_fmaf(head_sum(sum, a.lane_bits), a.by_dim, a.eps));
             scale_item<W>(x, weights + (kind == 0 ? 0 : a.head_dim), it, r);
-            if (it.pair >= 0) turn<W, PAIRS>(x, turn_of + t * a.padded + it.pair, it, a.half, exchange);
+            turn<W, PAIRS>(x, turn_of + t * a.padded, it, a, exchange);
         }
         store_item<T, W, STREAM>(dst, x, it);
     }
@@ -248,7 +265,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_any_kernel(NormArgs 
     float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim);
     const int t0 = blockIdx.x * a.per_block, here = min(a.per_block, a.tokens - t0);
     weights_to(weights, a);
-    turns_to<false>(turn_of, a, t0, here);
+    turns_to<0>(turn_of, a, t0, here);
     __syncthreads();
     const int lane = threadIdx.x & 63;
     const uint32_t rows = (uint32_t)here * (a.Hq + (PAGES ? 2 : 1) * a.Hkv);
@@ -293,7 +310,7 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const void* x_b
         float x[2 * W], g[2 * W];
         load_item<T, W, STREAM>(x, static_cast<const T*>(x_base) + token * st + h * sh, it);
         load_item<T, W, STREAM>(g, static_cast<const T*>(g_base) + token * go_st + h * go_sh, it);
-        if (it.pair >= 0) turn<W, PAIRS>(g, turn_of + t * a.padded + it.pair, it, a.half, exchange);
+        turn<W, PAIRS>(g, turn_of + t * a.padded, it, a, exchange);
         float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 2 * W; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
@@ -321,15 +338,15 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormArgs a)
     constexpr int W = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char norm_lds[];
     float* const weights = reinterpret_cast<float*>(norm_lds);
-    float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> 6) * 2 * W * 64;
-    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * W : 0));
+    float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> a.lane_bits << a.lane_bits) * 2 * (W + 1);
+    float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * (W + 1) : 0));
     const int lane = threadIdx.x & ((1 << a.lane_bits) - 1);
     const Item it = item_of<T, PAIRS>(a, lane);
     float acc_q[2 * W] = {}, acc_k[2 * W] = {};
     weights_to(weights, a);
     for (int t0 = blockIdx.x * a.per_step; t0 < a.tokens; t0 += gridDim.x * a.per_step) {
         const int here = min(a.per_step, a.tokens - t0);
-        turns_to<PAIRS == kAcross>(turn_of, a, t0, here);
+        turns_to<PAIRS == kAcross ? W : 0>(turn_of, a, t0, here);
         __syncthreads();
         if (a.Hq > 0)
             backward_rows<T, PAIRS, STREAM>(a, a.q, a.gq, a.q_out, a.q_st, a.q_sh, a.qo_st, a.qo_sh, a.Hq, a.by_q, weights, turn_of, exchange,
@@ -374,7 +391,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_any_kernel(NormArg
     for (int i = threadIdx.x; i < kWaves * 2 * a.head_dim; i += kNormThreads) sums[i] = 0.f;
     for (int t0 = blockIdx.x * a.per_step; t0 < a.tokens; t0 += gridDim.x * a.per_step) {
         const int here = min(a.per_step, a.tokens - t0);
-        turns_to<false>(turn_of, a, t0, here);
+        turns_to<0>(turn_of, a, t0, here);
         __syncthreads();
         const uint32_t rows = (uint32_t)here * (a.Hq + a.Hkv);
         for (uint32_t row = wave; row < rows; row += kWaves) {
@@ -485,10 +502,10 @@ static bool arguments_of(const NormCall& c, NormArgs& a, Pairs& pairs) {
     a.eps = c.norm.eps, a.weight_offset = c.norm.weight_offset, a.by_dim = 1.f / s.head_dim, a.weight_dtype = c.norm.weight_dtype;
     a.tokens = s.tokens, a.Hq = s.num_q_heads, a.Hkv = s.num_kv_heads, a.half = s.rotary_dim / 2, a.head_dim = s.head_dim;
     pairs = !half_layout ? kNeighbours : a.half % W == 0 ? kHalves : kAcross;
-    a.turning = (s.rotary_dim + 2 * W - 1) / (2 * W);  // (kHalves: whole chunks of either half)
+    a.turning = a.half / W;                            // (of kHalves: whole chunks of either half)
     a.items = (s.head_dim + 2 * W - 1) / (2 * W);
     const bool wide = a.items <= 64;
-    a.padded = !wide ? a.half : pairs == kAcross ? spread(a.half - 1) + 1 : a.turning * W;
+    a.padded = !wide ? a.half : pairs == kAcross ? 2 * a.items * (W + 1) : (a.half + W / 2 - 1) / (W / 2) * (W / 2);    // (of whole chunks)
     a.lane_bits = 2;
     while (1 << a.lane_bits < a.items && a.lane_bits < 6) ++a.lane_bits;
     if (!wide) a.lane_bits = 6;
@@ -518,7 +535,7 @@ static int tokens_for(const NormArgs& a, int heads) {
 // LDS of the weights, of what lanes exchange, and of the (cos, sin) of per_step tokens
 template <typename T>
 static size_t lds_of(const NormArgs& a, bool exchanges) {
-    return sizeof(float) * (2 * a.head_dim + (exchanges ? kNormThreads * 2 * (16 / sizeof(T)) : 0)) + sizeof(float2) * (size_t)a.per_step * a.padded;
+    return sizeof(float) * (2 * a.head_dim + (exchanges ? kNormThreads * 2 * (16 / sizeof(T) + 1) : 0)) + sizeof(float2) * (size_t)a.per_step * a.padded;
 }
 
 template <typename T>
