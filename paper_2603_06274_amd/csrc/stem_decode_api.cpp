@@ -121,8 +121,22 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)(), bo
     // call of 8 requests: d = 64, 8 / 2 heads, 300 keys 8.2 / 11.1, 1000 9.3 / 11.1, 1500 10.5 / 11.1, 2000 11.8 / 11.2; d = 128, 32 / 8 heads, 240 keys 9.4 /
     // 11.1, 1040 14.5 / 11.5; d = 256, 140 keys 13.4 / 15.3 and for one request 13.6 / 10.9.  (The prefix within 32-bit byte offsets, too.)
     const int64_t most_small = s.head_dim == 64 ? 1536 : s.head_dim == 128 ? 384 : -1;
-    p.small = own_rows <= 16 && (int64_t)s.requests * s.num_kv_heads <= units_here && (int64_t)s.prefix_len + s.max_suffix <= most_small &&
-              (s.prefix_len == 0 || ((int64_t)s.prefix_len + 127) / 128 * 128 * s.prefix_stride_token * 2 <= kInt32Max);
+    const int64_t small_keys = (int64_t)s.prefix_len + s.max_suffix;
+    const bool near = s.prefix_len == 0 || ((int64_t)s.prefix_len + 127) / 128 * 128 * s.prefix_stride_token * 2 <= kInt32Max;
+    p.small = own_rows <= 16 && (int64_t)s.requests * s.num_kv_heads <= units_here && small_keys <= most_small && near;
+    if (tree && near) {
+        // Trees have more rows, in tiles of 64 (32 with d = 256), and with a workgroup for three CUs of eight, or several for a request, they are worth it
+        // for longer, as the parts that they would be joined from are many rows'.  One launch / two, us a call in a graph: 4 requests of 8 tokens, 32 / 8
+        // heads of 128, 64 keys 8.0 / 11.6, 272 10.1 / 11.8, 496 13.0 / 12.0; 32 of 16, 80 keys 9.3 / 17.1, 656 19.1 / 35.9, 1536 30.4 / 41.5, 1000 of a
+        // prefix 25.0 / 50.6; d = 64, 48 of 8, 304 keys 11.9 / 15.5, 1024 25.0 / 24.4; d = 256, 8 of 8, 64 keys 11.2 / 15.8, 496 21.9 / 17.9, 24 of 12, 976
+        // 37.7 / 38.6; four workgroups per CU 32.7 / 28.2.  Of 16 rows, 32 of 2 and 128 values, 720 keys 15.2 / 21.7, 1536 24.9 / 27.6.
+        const int tile = own_rows <= 16 && s.head_dim <= 128 ? 16 : s.head_dim == 256 ? 32 : 64;
+        const int64_t tiles = (own_rows + tile - 1) / tile, workgroups = s.requests * tiles * s.num_kv_heads;
+        const bool many = 8 * workgroups >= 3 * units_here || (tiles > 1 && s.head_dim != 256);
+        const int64_t most = tile == 16 && s.head_dim == 64 ? most_small : many ? (s.head_dim == 128 ? 1536 : 1024) : s.head_dim == 256 ? 256 : 384;
+        p.small = workgroups <= 2 * units_here && small_keys <= most;
+        if (p.small) p.suffix_row_tile = tile, p.suffix_row_tiles = (int32_t)tiles;
+    }
     if (p.small) p.prefix_splits = p.suffix_splits = 0;
     p.prefix_groups = ((int64_t)s.num_kv_heads * p.prefix_splits + 7) / 8 * 8 * p.row_tiles;
     p.groups = p.prefix_groups + p.own_slots * s.num_kv_heads * p.suffix_splits;

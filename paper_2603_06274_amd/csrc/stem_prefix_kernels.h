@@ -744,23 +744,25 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
 }
 
-// Small calls in one launch: a workgroup has all keys of its request's rows, the prefix's (which are read once per request then) and its own.
+// Small calls in one launch: a workgroup has all keys of a row tile of its request, the prefix's (which are read once per tile then) and its own.
 template <typename T, int D, typename S, bool TREE>
 __global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a) {
     using P = Part<T, D, S>;
     __shared__ __align__(1024) unsigned char lds[P::kLds];
     __shared__ float2 wave_ml[S::kRows * S::KW];
-    const int g = blockIdx.x % a.Hkv, r = blockIdx.x / a.Hkv;
+    const int g = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv;
+    const int r = S::RW == 1 ? slot : slot / a.suffix_row_tiles, m0 = S::RW == 1 ? 0 : (slot - r * a.suffix_row_tiles) * S::kRows;
     int first, n;
     new_tokens(a, r, first, n);
     const int mine = min(n, a.max_new) * a.G;
-    if (mine <= 0) return;
+    if (m0 >= mine) return;
     P t;
-    t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, 0, mine);
+    t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, m0, mine);
     if (a.prefix_len > 0) walk_prefix<S>(t, a, g, 0, a.prefix_len, lds);
     const int len = suffix_len(a, r);
-    if (len > 0) walk_own<T, TREE, S>(t, a, r, g, first, n, len, 0, len, 0, mine, lds);
-    t.finish_rows(lds, wave_ml, a, first, g, 0, mine);
+    if (S::RW > 1 && a.prefix_len > 0) STEM_LDS_BARRIER();         // no wave is in a tile of the prefix any more
+    if (len > 0) walk_own<T, TREE, S>(t, a, r, g, first, n, len, 0, len, m0, mine, lds);
+    t.finish_rows(lds, wave_ml, a, first, g, m0, mine);
 }
 
 // Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
@@ -776,8 +778,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
     int r = 0, i = 0, h = 0, first = 0, n = 0, parts = 0;
     bool mine = false;                                 // whether the row is one of a request's
     if constexpr (BY_ROWS) {                           // token, head
-        constexpr int kWaveRows = GROUPS > 1 ? 1 : 64 / kLanes;   // different rows of a wave
-        const uint32_t wave0 = GROUPS > 1 ? item0 : item0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kWaveRows;
+        constexpr int kRowLanes = kLanes * GROUPS, kWaveRows = kRowLanes < 64 ? 64 / kRowLanes : 1;   // different rows of a wave
+        const uint32_t wave0 = item0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 / kRowLanes;
         int known = -1, owner = -1;
 #pragma unroll
         for (int x = 0; x < kWaveRows; ++x) {
@@ -863,19 +865,29 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
     using Rows32 = Split<1, 2, W / 2>;
     using Rows64 = Split<2, 2, W / 2>;
     using Rows128 = Split<2, 4, W / 4>;
+    if constexpr (TREE)
+        if (p.small && p.suffix_row_tile > 16) {
+            using Small = Split<1, D == 256 ? 2 : 4, 2>;
+            hipLaunchKernelGGL((small_attn_kernel<T, D, Small, TREE>), dim3((unsigned)(a.requests * a.suffix_row_tiles * a.Hkv)),
+                               dim3(64 * Small::kWaves), 0, stream, a);
+            return check_launch();
+        }
     if constexpr (D != 256)
         if (p.small) {
             using Small = Split<1, 1, D == 64 ? 8 : 4>;
             hipLaunchKernelGGL((small_attn_kernel<T, D, Small, TREE>), dim3((unsigned)(a.requests * a.Hkv)), dim3(64 * Small::kWaves), 0, stream, a);
             return check_launch();
         }
-    // several groups of lanes per row where there are parts for them
-    constexpr int kGroups = 4 * kJoinThreads / D;
+    // Several groups of lanes per row where there are parts for them, a workgroup's with one token per request.  Trees have many rows: two groups
+    // each.  1 / 2 / a whole workgroup's: 254 / 254 / 262 us (16 requests of up to 32 drafts and 32768 tokens, 32 / 8 heads), 44 / 41 / 52 (48 of 8 behind
+    // 2000), 29 / 30 / 39 (the same with d = 64), 22.7 / 19.5 / 19.7 (one of 8, 32768), 15.3 / 14.1 / 14.3 (4 of 8, 2000).
+    constexpr int kLanes = D / 4, kGroups = TREE ? 2 : kJoinThreads / kLanes, kRowLanes = kJoinThreads / kLanes;
     const bool many = p.prefix_splits + p.suffix_splits > 4;
+    const int joined = many ? kRowLanes / kGroups : kRowLanes;    // rows of a workgroup
     // (a line of a grid has less than 2^32 threads, and where there are lines each begins with a workgroup of XCD 0)
     constexpr int64_t kLine = 1 << kLineBits;
     auto grid_of = [](int64_t n) { return n <= kLine ? dim3((unsigned)n) : dim3((unsigned)kLine, (unsigned)((n + kLine - 1) >> kLineBits)); };
-    const dim3 grid = grid_of(p.groups), joins = grid_of(many ? p.join_rows : (p.join_rows + kGroups - 1) / kGroups);
+    const dim3 grid = grid_of(p.groups), joins = grid_of((p.join_rows + joined - 1) / joined);
     if (p.groups > 0) {
 #define STEM_PREFIX_LAUNCH(SP, SO) \
     hipLaunchKernelGGL((prefix_attn_kernel<T, D, SP, SO, TREE>), grid, dim3(64 * SP::kWaves), 0, stream, a)

@@ -262,8 +262,9 @@ def test_the_split_covers_all_own_keys_within_its_workspace():
                         tile, tiles, splits, least, prefix_splits, slots, ml, size, small, groups = list(out)
                         own = min(max_new * G, tokens * G)
                         assert tile * (tiles - 1) < own <= tile * tiles
-                        if small:
-                            assert splits == prefix_splits == 0 and tile == 16 and tiles == 1
+                        if small:                  # one launch, a workgroup for each row tile of a request
+                            assert splits == prefix_splits == 0 and requests * tiles * hkv <= 512 and prefix_len + suffix <= 1536
+                            assert tile == (16 if own <= 16 and d != 256 else 32 if d == 256 else 64)
                             continue
                         assert 1 <= splits <= 64 and slots >= min(requests * tiles, requests + tokens * G // tile)
                         n = (splits + prefix_splits) * hkv * tokens * G
