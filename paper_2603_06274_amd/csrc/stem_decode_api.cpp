@@ -130,7 +130,10 @@ int prefix_plan(const stem_prefix_shape& s, PrefixPlan* plan, int (*units)(), bo
         // heads of 128, 64 keys 8.0 / 11.6, 272 10.1 / 11.8, 496 13.0 / 12.0; 32 of 16, 80 keys 9.3 / 17.1, 656 19.1 / 35.9, 1536 30.4 / 41.5, 1000 of a
         // prefix 25.0 / 50.6; d = 64, 48 of 8, 304 keys 11.9 / 15.5, 1024 25.0 / 24.4; d = 256, 8 of 8, 64 keys 11.2 / 15.8, 496 21.9 / 17.9, 24 of 12, 976
         // 37.7 / 38.6; four workgroups per CU 32.7 / 28.2.  Of 16 rows, 32 of 2 and 128 values, 720 keys 15.2 / 21.7, 1536 24.9 / 27.6.
-        const int tile = own_rows <= 16 && s.head_dim <= 128 ? 16 : s.head_dim == 256 ? 32 : 64;
+        // With d = 64 and more than 320 keys, 16 rows each, whose eight waves share the keys and wait for no other, as long as there are CUs for them:
+        // 4 of 16, 8 / 2 heads, 640 keys 8.6 / 10.5, 1000 of a prefix 10.6 / 13.3; 8 of 8, 32 / 8 heads, 1232 13.1 / 14.2; two a CU 25.1 / 19.0.
+        const bool narrow = s.head_dim == 64 && small_keys > 320 && 2 * ((own_rows + 15) / 16) * s.requests * s.num_kv_heads <= units_here;
+        const int tile = narrow || (own_rows <= 16 && s.head_dim <= 128) ? 16 : s.head_dim == 256 ? 32 : 64;
         const int64_t tiles = (own_rows + tile - 1) / tile, workgroups = s.requests * tiles * s.num_kv_heads;
         const bool many = 8 * workgroups >= 3 * units_here || (tiles > 1 && s.head_dim != 256);
         const int64_t most = tile == 16 && s.head_dim == 64 ? most_small : many ? (s.head_dim == 128 ? 1536 : 1024) : s.head_dim == 256 ? 256 : 384;

@@ -751,7 +751,7 @@ __global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a
     __shared__ __align__(1024) unsigned char lds[P::kLds];
     __shared__ float2 wave_ml[S::kRows * S::KW];
     const int g = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv;
-    const int r = S::RW == 1 ? slot : slot / a.suffix_row_tiles, m0 = S::RW == 1 ? 0 : (slot - r * a.suffix_row_tiles) * S::kRows;
+    const int r = TREE ? slot / a.suffix_row_tiles : slot, m0 = TREE ? (slot - r * a.suffix_row_tiles) * S::kRows : 0;
     int first, n;
     new_tokens(a, r, first, n);
     const int mine = min(n, a.max_new) * a.G;
@@ -875,7 +875,8 @@ static int launch(const PrefixArgs& a, const PrefixPlan& p, hipStream_t stream) 
     if constexpr (D != 256)
         if (p.small) {
             using Small = Split<1, 1, D == 64 ? 8 : 4>;
-            hipLaunchKernelGGL((small_attn_kernel<T, D, Small, TREE>), dim3((unsigned)(a.requests * a.Hkv)), dim3(64 * Small::kWaves), 0, stream, a);
+            hipLaunchKernelGGL((small_attn_kernel<T, D, Small, TREE>), dim3((unsigned)(a.requests * (TREE ? a.suffix_row_tiles : 1) * a.Hkv)),
+                               dim3(64 * Small::kWaves), 0, stream, a);
             return check_launch();
         }
     // Several groups of lanes per row where there are parts for them, a workgroup's with one token per request.  Trees have many rows: two groups
