@@ -10,7 +10,7 @@
 // time, a workgroup a few tokens, whose (cos, sin) it computes once, beside the weights, into LDS.
 //
 // Halves that do not both begin at 16 bytes lie in the lanes as they lie in memory, and are exchanged through LDS: 16-bit values are bound by
-// that and its places (16384 tokens of 32 + 8 heads of 128, 50 values of each turning, bf16: 105 us, backwards 173; 48 values: 74 and 124;
+// that and its places (16384 tokens of 32 + 8 heads of 128, 50 values of each turning, bf16: 72 us, backwards 173; 48 values: 74 and 124;
 // fp32 values: 110 and 178, as fast as memory; one pair of values per lane at a time, as below: 312 and 674 in bf16).  Heads that are longer
 // than 64 lanes hold (fp32 beyond 512 values) go one wave each, a pair of values per lane at a time, read twice (the second time from the caches).
 #include "stem_rotary_common.h"
@@ -569,7 +569,13 @@ int launch_norm_rotary(const NormCall& c, hipStream_t stream) {
     Pairs pairs;
     const bool wide = arguments_of(c, a, pairs), pages = c.rotary.slots != nullptr;
     const int heads = a.Hq + (pages ? 2 : 1) * a.Hkv;
-    a.per_block = a.per_step = tokens_for(a, heads);
+    // A long call's workgroups take two tokens where they would take one, four if lanes exchange halves: the vector instructions of 16-bit
+    // values fill 75 % of the time of one (weights, (cos, sin) and partly idle waves for 40 heads).  1 / 2 / 4 tokens: 131072 of 32 + 8 heads of 128
+    // 468 / 451 / 466 us (four read from further apart), 16384 with 50 values turning 96 / 78 / 72, in fp32 109 / 113 / 123.
+    a.per_block = tokens_for(a, heads);
+    const int most = s.dtype == STEM_FP32 ? 1 : pairs == kAcross ? 4 : 2;
+    while (2 * a.per_block <= most && s.tokens / (2 * a.per_block) >= 4096 && 2 * a.per_block * a.padded <= kNormPairs) a.per_block *= 2;
+    a.per_step = a.per_block;
     const bool through = (int64_t)s.tokens * heads * s.head_dim * value_bytes(s.dtype) > 64 << 20;
     if (s.dtype == STEM_BF16) launch_forward<__bf16>(a, wide, pairs, pages, through, stream);
     else if (s.dtype == STEM_FP16) launch_forward<_Float16>(a, wide, pairs, pages, through, stream);

@@ -74,3 +74,31 @@ def test_new_tokens(dtype, d, rot):
     rest[slots[at].long()] = False
     assert (kp.cpu().view(-1, Hkv, d)[rest] == 9.0).all() and (vp.cpu().view(-1, Hkv, d)[rest] == 9.0).all()
     assert (q_out.cpu()[~at] == 9.0).all()
+
+
+@pytest.mark.parametrize("layout,rot", [("half", 128), ("half", 50), ("interleaved", 64)])
+def test_long_calls(layout, rot):
+    """Workgroups of several tokens, the last of them with fewer."""
+    g = torch.Generator().manual_seed(rot)
+    T, Hq, Hkv, d = 16387, 33, 4, 128
+    q, k = (torch.randn(T, h, d, generator=g).to(BF) for h in (Hq, Hkv))
+    pos = torch.randint(0, 1 << 20, (T,), generator=g).to(torch.int32)
+    turns, factor = db.stem_rotary_frequencies(rot, 10000.0)
+    ws = ws_of(g, d)
+    x = [t.to(DEV) for t in (q, k)]
+    out = [torch.full_like(t, float("nan")) for t in x]
+    nb.stem_norm_rotary(db.RotaryShape.from_tensors(*x, rot, layout), nb.HeadNorm(*(w.to(DEV) for w in ws), EPS, 0.0), *x, pos.to(DEV),
+                        turns.to(DEV), factor, *out)
+    some = torch.cat([torch.arange(9), torch.arange(8000, 8009), torch.arange(T - 9, T)])
+    for t, w, y in zip((q, k), ws, out):
+        assert y.isfinite().all()
+        want, bound = nu.norm_reference(t[some], w, 0.0, EPS, pos[some], turns, factor, rot, layout)
+        assert ((y.cpu()[some].double() - want).abs() <= bound).all()
+    # every row as in short calls
+    for lo in range(0, T, 4000):
+        part = [t[lo:lo + 4000] for t in x]
+        again = [torch.empty_like(t) for t in part]
+        nb.stem_norm_rotary(db.RotaryShape.from_tensors(*part, rot, layout), nb.HeadNorm(*(w.to(DEV) for w in ws), EPS, 0.0), *part,
+                            pos[lo:lo + 4000].to(DEV), turns.to(DEV), factor, *again)
+        for y, z in zip(out, again):
+            assert torch.equal(y[lo:lo + 4000], z)
