@@ -779,7 +779,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
     bool mine = false;                                 // whether the row is one of a request's
     if constexpr (BY_ROWS) {                           // token, head
         constexpr int kRowLanes = kLanes * GROUPS, kWaveRows = kRowLanes < 64 ? 64 / kRowLanes : 1;   // different rows of a wave
-        const uint32_t wave0 = item0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 / kRowLanes;
+        const uint32_t wave0 = kRowLanes == kJoinThreads ? item0 : item0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64 / kRowLanes;
         int known = -1, owner = -1;
 #pragma unroll
         for (int x = 0; x < kWaveRows; ++x) {
