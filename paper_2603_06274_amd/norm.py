@@ -59,7 +59,7 @@ class NormRotary(Rotary):
     def none(cls, head_dim: int, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
              weight_offset: float = 0.0, device="cuda") -> "NormRotary":
         """Norms without positions."""
-        r = cls(head_dim, q_weight, k_weight, eps, weight_offset, 2, device)
+        r = cls(head_dim, q_weight, k_weight, eps, weight_offset, 2, device, layout="interleaved")    # (a pair that does not leave its chunk)
         r.turns.zero_()
         return r
 

@@ -102,3 +102,15 @@ def test_long_calls(layout, rot):
                             pos[lo:lo + 4000].to(DEV), turns.to(DEV), factor, *again)
         for y, z in zip(out, again):
             assert torch.equal(y[lo:lo + 4000], z)
+
+
+def test_norms_without_positions():
+    from paper_2603_06274_amd.norm import NormRotary
+    g = torch.Generator().manual_seed(1)
+    q, k = (torch.randn(40, h, 64, generator=g).to(BF) for h in (5, 2))
+    ws = ws_of(g, 64)
+    r = NormRotary.none(64, *(w.to(DEV) for w in ws), EPS)
+    out = r.apply(q.to(DEV), k.to(DEV), torch.randint(0, 1 << 30, (40,), generator=g).to(torch.int32).to(DEV))
+    for x, w, y in zip((q, k), ws, out):
+        want, bound = nu.norm_reference(x, w, 0.0, EPS, torch.zeros(40, dtype=torch.int32), torch.zeros(1, dtype=torch.float64), 1.0, 2, "half")
+        assert ((y.cpu().double() - want).abs() <= bound).all()
