@@ -765,6 +765,17 @@ __global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a
     t.finish_rows(lds, wave_ml, a, first, g, m0, mine);
 }
 
+// c times a part's sums, or those of some of its waves.  Where c has become 0 what is finite is gone, and what is not stays: a row's weights are
+// more than 0, however small.  (Of trees, whose sums have only what the row sees that is not finite.)
+__device__ __forceinline__ f32x4_t carried(f32x4_t o, float c) {
+    f32x4_t y = o * c;
+    if (c == 0.f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __builtin_isfinite(o[e]) ? 0.f : o[e];
+    }
+    return y;
+}
+
 // Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
 // at a time is asked for before any of it is used, as a row waits for memory and does next to nothing else.
 constexpr int kJoinThreads = 256;
@@ -828,9 +839,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         o *= then;
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x) {
-            const float c = p0 + x * GROUPS < parts ? __builtin_amdgcn_exp2f(ml[x].x - top) : 0.f;
+            const bool there = p0 + x * GROUPS < parts;
+            const float c = there ? __builtin_amdgcn_exp2f(ml[x].x - top) : 0.f;
             l += c * ml[x].y;
-            if (c != 0.f) o += c * part[x];            // (0 times a part that is not finite is nothing of this row's)
+            if constexpr (TREE) {
+                if (there) o += carried(part[x], c);
+            } else {
+                if (c != 0.f) o += c * part[x];        // (0 times a part that is not finite is nothing of this row's)
+            }
         }
         m = top;
     }
