@@ -153,6 +153,18 @@ __device__ __forceinline__ void write_row(const PrefixArgs& a, int token, int he
         a.lse[(int64_t)head * a.tokens + token] = empty ? -__builtin_huge_valf() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// c times a part's sums, or those of some of its waves.  Where c has become 0 what is finite is gone, and what is not stays: a row's weights are
+// more than 0, however small.  (Of trees, whose sums have only what the row sees that is not finite.)
+template <bool TREE>
+__device__ __forceinline__ f32x4_t carried(f32x4_t o, float c) {
+    f32x4_t y = o * c;
+    if (TREE && c == 0.f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __builtin_isfinite(o[e]) ? 0.f : o[e];
+    }
+    return y;
+}
+
 // How the waves of a workgroup share its rows and keys: RW groups of 16 NQ rows times KW groups of 32 keys.  With RW = 1 every wave has
 // keys of its own and waits for no other; with RW > 1 the tile of 32 KW keys in LDS is read by RW waves each, and there are two
 // of them in turn, with a barrier per tile.
@@ -461,6 +473,7 @@ struct Part {
     }
 
     // The waves' results together -> the rows' outputs, where there are no other parts.  Row m0 of m_end is row m0 of token `first`.
+    template <bool TREE>
     __device__ __forceinline__ void finish_rows(unsigned char* lds, float2* wave_ml, const PrefixArgs& a, int first, int g, int m0, int m_end) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
 #pragma unroll
@@ -479,7 +492,7 @@ struct Part {
             const float mine = __builtin_amdgcn_exp2f(-off[n] - m);
             float* dst = reinterpret_cast<float*>(lds) + (kw * S::kRows + row) * D + 4 * grp;
 #pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[dt][n] * mine;
+            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = carried<TREE>(o[dt][n], mine);
         }
         __syncthreads();
         for (int x = threadIdx.x; x < S::kRows * D / 4; x += 64 * kWaves) {
@@ -501,6 +514,7 @@ struct Part {
     }
 
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
+    template <bool TREE>
     __device__ __forceinline__ void finish(unsigned char* lds, float2* wave_ml, float* part, float2* ml, int m0, int m_end) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
 #pragma unroll
@@ -541,7 +555,7 @@ struct Part {
             }
             float* dst = reinterpret_cast<float*>(lds) + (kw * S::kRows + row) * D + 4 * grp;
 #pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[dt][n] * mine;
+            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = carried<TREE>(o[dt][n], mine);
         }
         __syncthreads();
         for (int x = threadIdx.x; x < S::kRows * D / 4; x += 64 * kWaves) {
@@ -711,7 +725,7 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
         const int key0 = split * a.split_keys;
         walk_prefix<SP>(t, a, g, key0, min(a.split_keys, a.prefix_len - key0), lds);
         const int64_t place = ((int64_t)split * a.Hkv + g) * a.rows;
-        t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
+        t.template finish<TREE>(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
         return;
     }
     // a request's own keys
@@ -741,7 +755,7 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, m0, mine);
     walk_own<T, TREE, SO>(t, a, r, g, first, n, len, key0, keys, m0, mine, lds);
     const int64_t place = ((int64_t)(a.prefix_splits + split) * a.Hkv + g) * a.rows + (int64_t)first * a.G;
-    t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
+    t.template finish<TREE>(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
 }
 
 // Small calls in one launch: a workgroup has all keys of a row tile of its request, the prefix's (which are read once per tile then) and its own.
@@ -762,18 +776,7 @@ __global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a
     const int len = suffix_len(a, r);
     if (S::RW > 1 && a.prefix_len > 0) STEM_LDS_BARRIER();         // no wave is in a tile of the prefix any more
     if (len > 0) walk_own<T, TREE, S>(t, a, r, g, first, n, len, 0, len, m0, mine, lds);
-    t.finish_rows(lds, wave_ml, a, first, g, m0, mine);
-}
-
-// c times a part's sums, or those of some of its waves.  Where c has become 0 what is finite is gone, and what is not stays: a row's weights are
-// more than 0, however small.  (Of trees, whose sums have only what the row sees that is not finite.)
-__device__ __forceinline__ f32x4_t carried(f32x4_t o, float c) {
-    f32x4_t y = o * c;
-    if (c == 0.f) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = __builtin_isfinite(o[e]) ? 0.f : o[e];
-    }
-    return y;
+    t.template finish_rows<TREE>(lds, wave_ml, a, first, g, m0, mine);
 }
 
 // Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
@@ -836,14 +839,14 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         for (int x = 0; x < kAtOnce; ++x) top = fmaxf(top, ml[x].x);
         const float then = __builtin_amdgcn_exp2f(m - top);
         l *= then;
-        o *= then;
+        o = carried<TREE>(o, then);
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x) {
             const bool there = p0 + x * GROUPS < parts;
             const float c = there ? __builtin_amdgcn_exp2f(ml[x].x - top) : 0.f;
             l += c * ml[x].y;
             if constexpr (TREE) {
-                if (there) o += carried(part[x], c);
+                if (there) o += carried<TREE>(part[x], c);
             } else {
                 if (c != 0.f) o += c * part[x];        // (0 times a part that is not finite is nothing of this row's)
             }
@@ -860,13 +863,13 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         for (int x = 1; x < GROUPS; ++x) top = fmaxf(top, group_ml[my_row * GROUPS + x].x);
         const float mine = __builtin_amdgcn_exp2f(m - top);
         l *= mine;
-        o *= mine;
+        o = carried<TREE>(o, mine);
 #pragma unroll
         for (int x = 1; x < GROUPS; ++x) {
             const float2 other = group_ml[my_row * GROUPS + x];
             const float c = __builtin_amdgcn_exp2f(other.x - top);
             l += c * other.y;
-            o += c * group_o[threadIdx.x + x * kLanes];
+            o += carried<TREE>(group_o[threadIdx.x + x * kLanes], c);
         }
         m = top;
     }

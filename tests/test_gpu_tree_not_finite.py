@@ -1,5 +1,5 @@
-"""Values of new tokens that are not finite, where their weight is next to nothing: they reach the rows that see them all the same, in one launch
-and in two, whichever waves or parts have met the rows' other keys."""
+"""Values of new tokens that are not finite, where their weight is next to nothing: they reach the rows that see them all the same, an
+infinite one as itself, in one launch and in two, whichever waves or parts have met the rows' other keys."""
 import math
 
 import pytest
@@ -32,9 +32,24 @@ def check(c, j, value):
 
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("Hq,new", [(2, 40), (8, 40), (8, 70)])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_rows_of_which_some_waves_meet_no_key(dtype, d, Hq, new, value):
+    """Tokens that see themselves alone, in a request of no earlier ones."""
+    for room in (0, 20000):
+        c = with_room(TreeCase([0], [new], 0, Hq, 2, d, 16, dtype, seed=d), room)
+        c.masks[:] = 0
+        for t in range(new):
+            c.masks[t, t // 64] = 1 << (t % 64) if t % 64 < 63 else -(1 << 63)
+        for j in (2, 35, new - 1):
+            check(c, j, value)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("Hq,new", [(2, 6), (8, 20), (8, 70)])
 @pytest.mark.parametrize("place", ["prefix 0", "prefix 40", "own 5", "own 70", "own 590"])
-@pytest.mark.parametrize("value", [math.nan])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
 def test_beside_a_key_that_has_all_of_the_weight(dtype, d, Hq, new, place, value):
     """One earlier key's score is 250 above the others': their weights are 0 in 32 bits."""
     part, key = place.split()
