@@ -38,8 +38,6 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 256;
-// How pairs lie in a lane's values: neighbours; the two chunks; or one of them in another lane.
-enum Pairs { kNeighbours, kHalves, kAcross };
 constexpr int kNormPairs = 2048;                       // (cos, sin) that a workgroup holds at most
 
 // v_rsq_f32 is within 1 ulp; its argument is a normal number, as eps is one
@@ -90,32 +88,6 @@ __device__ __forceinline__ void turns_to(float2* turn_of, const NormArgs& a, int
     }
 }
 
-// What a lane has of a head: the chunks at `first` and `second`, W values each.  Neighbouring lanes have neighbouring chunks, so that a load or a
-// store of a wave is of whole lines (40961 tokens of 28 + 4 heads of 128, fp16, 64 values of each turning in neighbouring pairs: 118 us;
-// with 32 bytes in a row for a lane 157).
-struct Item {
-    int first, second, pair, second_pair;              // the chunks' first pairs, -1 if a chunk does not turn (kHalves: one for both)
-    bool has_first, has_second;
-};
-template <typename T, Pairs PAIRS>
-__device__ __forceinline__ Item item_of(const NormArgs& a, int i) {
-    constexpr int W = 16 / sizeof(T);
-    Item it;
-    if (PAIRS == kHalves) {                            // chunk i of the one half and of the other; behind them the others' two halves
-        const int rest = a.items - a.turning, x = i - a.turning;
-        it.first = i < a.turning ? i * W : 2 * a.half + x * W;
-        it.second = i < a.turning ? a.half + i * W : 2 * a.half + (rest + x) * W;
-        it.pair = it.second_pair = i < a.turning ? i * W : -1;
-    } else {
-        it.first = i * W, it.second = (a.items + i) * W;
-        it.pair = it.first < 2 * a.half ? it.first / 2 : -1;
-        it.second_pair = it.second < 2 * a.half ? it.second / 2 : -1;
-    }
-    it.has_first = i < a.items && it.first < a.head_dim;
-    it.has_second = i < a.items && it.second < a.head_dim;
-    return it;
-}
-
 // A lane's values turned, if any of them turn.  PAIRS says where the other of a pair is: in x[W + e], next to it, or in the lane that has the value
 // `half` further on or back.  cs: a token's (cos, sin).
 // exchange: the head's values for its other lanes, W + 1 places to a chunk (as in cs), so that one value of all lanes lies in different
@@ -144,7 +116,7 @@ __device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs, const 
         if (it.second_pair >= 0) chunk(x + W, cs + it.second_pair);
     } else {
         constexpr int S = W + 1;
-        const int half = a.half, shift = half / W, odd = half % W;
+        const int half = a.half;
         float* const mine[2] = {exchange + it.first / W * S, exchange + it.second / W * S};
         const float2* const turn_at[2] = {cs + it.first / W * S, cs + it.second / W * S};
 #pragma unroll
@@ -156,8 +128,7 @@ __device__ __forceinline__ void turn(float (&x)[2 * W], const float2* cs, const 
         float other[2 * W];
 #pragma unroll
         for (int e = 0; e < 2 * W; ++e) {              // (all asked for before any is used)
-            // `half` values further on and back, from the chunk's begin: the same for all lanes
-            const int y = e % W, on = shift * S + y + odd + (y + odd >= W), back = y - shift * S - odd - (y < odd);
+            const int y = e % W, on = place_on<W>(half, y), back = place_back<W>(half, y);
             const bool in_first = (e < W ? it.first : it.second) + y < half;
             other[e] = mine[e / W][in_first ? on : back];
             c[e] = turn_at[e / W][in_first ? y : back];
@@ -236,7 +207,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rotary_kernel(NormArgs a) {
     turns_to<PAIRS == kAcross ? W : 0>(turn_of, a, t0, here);
     __syncthreads();
     const int lane = threadIdx.x & ((1 << a.lane_bits) - 1);
-    const Item it = item_of<T, PAIRS>(a, lane);
+    const Item it = item_of<W, PAIRS>(a.items, a.turning, a.half, a.head_dim, lane);
     const uint32_t rows = (uint32_t)here * (a.Hq + (PAGES ? 2 : 1) * a.Hkv);
     for (uint32_t row = threadIdx.x >> a.lane_bits; row < rows; row += kNormThreads >> a.lane_bits) {
         const T* src;
@@ -341,7 +312,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormArgs a)
     float* const exchange = weights + 2 * a.head_dim + (threadIdx.x >> a.lane_bits << a.lane_bits) * 2 * (W + 1);
     float2* const turn_of = reinterpret_cast<float2*>(weights + 2 * a.head_dim + (PAIRS == kAcross ? kNormThreads * 2 * (W + 1) : 0));
     const int lane = threadIdx.x & ((1 << a.lane_bits) - 1);
-    const Item it = item_of<T, PAIRS>(a, lane);
+    const Item it = item_of<W, PAIRS>(a.items, a.turning, a.half, a.head_dim, lane);
     float acc_q[2 * W] = {}, acc_k[2 * W] = {};
     weights_to(weights, a);
     for (int t0 = blockIdx.x * a.per_step; t0 < a.tokens; t0 += gridDim.x * a.per_step) {
@@ -490,8 +461,7 @@ __global__ __launch_bounds__(kSumThreads) void norm_weights_kernel(const float* 
 static bool arguments_of(const NormCall& c, NormArgs& a, Pairs& pairs) {
     const RotaryCall& r = c.rotary;
     const stem_rotary_shape& s = r.shape;
-    const bool pages = r.slots != nullptr, half_layout = s.layout == STEM_ROTARY_HALF;
-    const int W = s.dtype == STEM_FP32 ? 4 : 8;
+    const bool pages = r.slots != nullptr;
     a = {};
     a.q = r.q, a.k = r.k, a.v = r.v, a.gq = c.grad_q, a.gk = c.grad_k;
     a.q_out = r.q_out, a.k_out = r.k_out, a.v_out = r.v_out;
@@ -501,14 +471,8 @@ static bool arguments_of(const NormCall& c, NormArgs& a, Pairs& pairs) {
     a.factor = r.factor, a.sine_factor = r.backward ? -r.factor : r.factor;
     a.eps = c.norm.eps, a.weight_offset = c.norm.weight_offset, a.by_dim = 1.f / s.head_dim, a.weight_dtype = c.norm.weight_dtype;
     a.tokens = s.tokens, a.Hq = s.num_q_heads, a.Hkv = s.num_kv_heads, a.half = s.rotary_dim / 2, a.head_dim = s.head_dim;
-    pairs = !half_layout ? kNeighbours : a.half % W == 0 ? kHalves : kAcross;
-    a.turning = a.half / W;                            // (of kHalves: whole chunks of either half)
-    a.items = (s.head_dim + 2 * W - 1) / (2 * W);
-    const bool wide = a.items <= 64;
-    a.padded = !wide ? a.half : pairs == kAcross ? 2 * a.items * (W + 1) : (a.half + W / 2 - 1) / (W / 2) * (W / 2);    // (of whole chunks)
-    a.lane_bits = 2;
-    while (1 << a.lane_bits < a.items && a.lane_bits < 6) ++a.lane_bits;
-    if (!wide) a.lane_bits = 6;
+    const HeadLayout l = head_layout(s);
+    pairs = l.pairs, a.items = l.items, a.turning = l.turning, a.lane_bits = l.lane_bits, a.padded = l.padded;
     const int heads = a.Hq + (pages ? 2 : 1) * a.Hkv;
     a.by_heads = fast_div(heads);
     a.by_q = fast_div(a.Hq > 0 ? a.Hq : 1), a.by_k = fast_div(a.Hkv > 0 ? a.Hkv : 1);
@@ -521,7 +485,7 @@ static bool arguments_of(const NormCall& c, NormArgs& a, Pairs& pairs) {
         a.page_mask = r.pages.page_size - 1;
         a.slots_end = (uint32_t)r.pages.num_pages * r.pages.page_size;
     }
-    return wide;
+    return l.in_registers;
 }
 
 // Tokens of which a workgroup's lanes have a head each, of `heads` per token; at most what its LDS has room for.
