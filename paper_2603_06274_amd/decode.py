@@ -136,12 +136,17 @@ class PagedCache:
         """Room for a step: new_lens int32 [requests] new tokens (None: one each; negative: the request has finished and its pages
         go back), each at most max_new (0: any number).  Brings lens, table, cu_new, positions and slots up to date; a step for which
         there is no room changes none of the first two, has no tokens and says so in status (see refused)."""
-        self.shape.c.max_new = max_new
+        c = self.shape.c
+        then, c.max_new = c.max_new, max_new
+        try:
+            db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
+                                self.cu_new, self.positions, self.slots, self.status, self.workspace)
+        except Exception:                                  # (no step has been taken: the one before is the last)
+            c.max_new = then
+            raise
         self._offset_open = False
         if self._step_open is not None:
             self._step_open = None if self._capturing() else True
-        db.stem_block_table(self.shape, self.lens, new_lens, self.ring_state, self.ring, self.table, self.lens, self.ring_state,
-                            self.cu_new, self.positions, self.slots, self.status, self.workspace)
 
     def begin_behind(self, length: int) -> None:
         """The requests' first position is `length`, unless another was given when the cache was made.  Raises if the cache has begun, or

@@ -1,0 +1,34 @@
+"""PagedCache.accept beside calls that are refused: what is open, and what is left as it was.  Without a GPU."""
+import pytest
+import torch
+
+from paper_2603_06274_amd import decode_binding as db
+from paper_2603_06274_amd import tree_binding as tb
+from paper_2603_06274_amd.decode import PagedCache
+
+from test_norm_tree_host import here, whole       # noqa: F401
+
+TABLE = db.stem_block_table
+
+
+@pytest.fixture
+def calls(here, monkeypatch):                     # noqa: F811
+    """What reaches the library."""
+    made = []
+    monkeypatch.setattr(db, "stem_block_table", lambda *a: made.append("table"))
+    monkeypatch.setattr(tb, "stem_tree_accept", lambda *a: made.append("accept"))
+    monkeypatch.setattr(tb, "stem_tree_commit", lambda *a: made.append("commit"))
+    return made
+
+
+def test_a_step_that_is_refused_opens_nothing(calls, monkeypatch):
+    cache, x = PagedCache(2, 4, 16, 2, 1, 64, tokens=4, device="cpu"), whole(4)
+    cache.advance(None, 2)
+    cache.accept(x, x, x)
+    monkeypatch.setattr(db, "stem_block_table", TABLE)
+    with pytest.raises(ValueError, match="new_lens"):
+        cache.advance(x.double(), 3)
+    assert cache.shape.c.max_new == 2
+    with pytest.raises(RuntimeError, match="no step"):
+        cache.accept(x, x, x)
+    assert calls == ["table", "accept", "commit"]
