@@ -11,7 +11,7 @@ from typing import Optional
 
 import torch
 
-from .decode_binding import (DTYPES, PageShape, PrefixShape, _check, _f32, _here, _i32, _lines, _need, _sz, _values, _vp, _whole,
+from .decode_binding import (DTYPES, STEM_MAX_HEAD_DIM, PageShape, PrefixShape, _check, _f32, _here, _i32, _lines, _need, _sz, _values, _vp, _whole,
                              lib as _decode_lib, stem_pages, stem_prefix_shape)
 
 STEM_MAX_TREE = 1024
@@ -130,6 +130,13 @@ def stem_tree_accept(shape: AcceptShape, parents: torch.Tensor, draft_ids: torch
         _whole(lens_out, R, "lens_out", dev), _whole(ring_state_out, 2, "ring_state_out", dev), _whole(accepted, R, "accepted", dev),
         _whole(path, T, "path", dev), _whole(next_ids, R, "next_ids", dev, ids), _whole(status, 2, "status", dev),
         _whole(workspace, 0, "workspace", dev, torch.uint8), workspace.numel(), stream), "stem_tree_accept")
+
+
+def need_movable_rows(pages: PageShape) -> None:
+    """What stem_tree_commit asks of pages beyond what their block table does: types and sizes of rows."""
+    d, dtype = pages.head_dim, pages.seen[2]
+    if dtype not in DTYPES or d % 8 or d > STEM_MAX_HEAD_DIM or pages.heads < 1 or pages.heads * d * dtype.itemsize > 1 << 26:
+        raise ValueError("rows of %d heads of %d values of %s cannot be moved" % (pages.heads, d, dtype))
 
 
 def stem_tree_commit(shape: AcceptShape, pages: PageShape, path: torch.Tensor, slots: torch.Tensor, cu_new: torch.Tensor,

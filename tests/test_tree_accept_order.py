@@ -32,3 +32,15 @@ def test_a_step_that_is_refused_opens_nothing(calls, monkeypatch):
     with pytest.raises(RuntimeError, match="no step"):
         cache.accept(x, x, x)
     assert calls == ["table", "accept", "commit"]
+
+
+@pytest.mark.parametrize("d,heads,dtype", [(100, 1, torch.bfloat16), (1032, 1, torch.bfloat16), (64, 1, torch.float64),
+                                           (1024, 32769, torch.bfloat16), (1024, 16385, torch.float32)])
+def test_pages_whose_rows_cannot_be_moved(calls, d, heads, dtype):
+    """Refused before the books change."""
+    cache, x = PagedCache(2, 4, 16, 2, 1, d, tokens=4, dtype=dtype, device="cpu"), whole(4)
+    cache.pages.heads = heads                     # (rows of 64 MiB and more, without their memory)
+    cache.advance(None, 2)
+    with pytest.raises(ValueError, match="moved"):
+        cache.accept(x, x, x)
+    assert calls == ["table"]
