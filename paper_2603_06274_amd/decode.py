@@ -171,9 +171,8 @@ class PagedCache:
         was drafted: a request's first one, and behind a kept one the draft that is the model's own choice there.  draft_ids and target_ids
         (int32 or int64 [tokens]): the token in each row, and the model's choice behind it.  Brings lengths and free pages up to date and
         moves the kept tokens' keys and values up; once per step (a second time raises, unless steps are replayed from a graph, where nobody
-        sees it).  Returns (accepted int32 [requests], path int32 [tokens], next_ids
-        [requests]), as stem_tree_accept has them, in buffers of the cache.  What cannot be done changes nothing and shows in
-        accept_refused."""
+        sees it).  Returns (accepted int32 [requests], path int32 [tokens], next_ids [requests]), as stem_tree_accept has them, in buffers of
+        the cache.  What cannot be done changes nothing and shows in accept_refused, after which it can be tried again."""
         capturing = self._capturing()                      # (of the step before a replay, whichever that will be)
         if self._step_open is False and not capturing:
             raise RuntimeError("there is no step of which anything could be accepted")
@@ -195,8 +194,11 @@ class PagedCache:
 
     def accept_refused(self) -> Tuple[int, int]:
         """Why the last accept was refused, if it was: requests with unusable numbers of tokens; room for pages given back.  Waits for the
-        GPU."""
-        return tuple(self.accept_status.tolist())
+        GPU.  A step whose acceptance was refused is open again then."""
+        why = tuple(self.accept_status.tolist())
+        if any(why) and self._step_open is False:
+            self._step_open = True
+        return why
 
     def _rows_shape(self, rotary: Rotary, q, k, v, q_out) -> db.RotaryShape:
         """The shape of a step's rows.  Raises unless they go with the cache and with each other."""

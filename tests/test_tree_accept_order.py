@@ -44,3 +44,23 @@ def test_pages_whose_rows_cannot_be_moved(calls, d, heads, dtype):
     with pytest.raises(ValueError, match="moved"):
         cache.accept(x, x, x)
     assert calls == ["table"]
+
+
+def test_a_refused_acceptance_can_be_tried_again(calls):
+    """Once accept_refused has said that it was refused, and only then."""
+    cache, x = PagedCache(2, 4, 16, 2, 1, 64, tokens=4, device="cpu"), whole(4)
+    assert cache.accept_refused() == (0, 0)
+    with pytest.raises(RuntimeError):
+        cache.accept(x, x, x)                     # (there is no step)
+    for why in ((1, 0), (0, 2)):
+        cache.advance(None, 2)
+        cache.accept(x, x, x)
+        cache.accept_status.copy_(torch.tensor(why))
+        with pytest.raises(RuntimeError):
+            cache.accept(x, x, x)                 # (nobody has asked)
+        assert cache.accept_refused() == why
+        cache.accept(x, x, x)
+        cache.accept_status.zero_()
+        assert cache.accept_refused() == (0, 0)
+        with pytest.raises(RuntimeError):
+            cache.accept(x, x, x)
