@@ -100,7 +100,13 @@ def build(extra_flags=(), verbose: bool = True) -> str:
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 2)) as ex:
         checked, tensors = ex.submit(check_wait_states, list(extra_flags)), ex.submit(build_tensors)
         objs = list(ex.map(lambda s: _compile(s, list(extra_flags)), SOURCES))
-        checked.result(), tensors.result()
+        checked.result()
+        try:
+            tensors.result()
+        except Exception as e:                          # (the bindings have the same checks in Python)
+            sys.stderr.write("the bindings will check tensors in Python, which takes longer: %s\n" % e)
+            if os.path.exists(TENSORS):
+                os.remove(TENSORS)
     cmd = [hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", LIB]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
