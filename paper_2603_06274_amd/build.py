@@ -8,6 +8,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -15,7 +16,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libstem_hip.so")
-TENSORS = os.path.join(PKG, "_tensors.so")               # the bindings' checks of tensors, for this Python and this torch
+# the bindings' checks of tensors: for this Python, which finds no other's under this name, and for this torch, which the module asks for itself
+TENSORS = os.path.join(PKG, "_tensors" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 SOURCES = ["stem_api.cpp", "stem_pool.hip", "stem_scores.hip", "stem_select.hip", "stem_attn.hip", "stem_static.hip",
            "stem_decode_api.cpp", "stem_rotary.hip", "stem_table.hip", "stem_prefix.hip", "stem_norm_api.cpp", "stem_norm.hip",
@@ -58,16 +60,16 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
-def build_tensors() -> None:
-    """The Python module of csrc/tensors_module.cpp: host code alone, against torch's headers and libraries."""
-    import sysconfig
-
+def build_tensors(made_for: str = "") -> None:
+    """The Python module of csrc/tensors_module.cpp: host code alone, against torch's headers and libraries.  made_for: the torch that it says
+    it is for, "version commit" (the one that is here)."""
     import torch
     from torch.utils import cpp_extension
+    made_for = made_for or "%s %s" % (torch.__version__, torch.version.git_version)
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     includes = [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]
     cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(), *("-isystem" + x for x in includes),
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(), '-DSTEM_TORCH="%s"' % made_for, *("-isystem" + x for x in includes),
            os.path.join(CSRC, "tensors_module.cpp"), "-L" + libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", TENSORS]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
@@ -107,6 +109,8 @@ def build(extra_flags=(), verbose: bool = True) -> str:
             sys.stderr.write("the bindings will check tensors in Python, which takes longer: %s\n" % e)
             if os.path.exists(TENSORS):
                 os.remove(TENSORS)
+        if os.path.exists(os.path.join(os.path.dirname(TENSORS), "_tensors.so")):      # (as it was called before, for any Python)
+            os.remove(os.path.join(os.path.dirname(TENSORS), "_tensors.so"))
     cmd = [hipcc(), "-shared", "-fPIC", "--offload-arch=gfx950", *objs, "-o", LIB]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

@@ -1,8 +1,11 @@
 // The bindings' checks of a call's tensors, as a Python module: type, sizes, strides and device of a torch tensor are read where they are,
 // not through five methods of the interpreter each (0.1 instead of 0.5 us a tensor, of which a call has 5 to 15 and a small kernel takes 3).
 // A tensor that is what it has to be gives its address; whatever is not goes to the Python function of the same name, which says why.
+// STEM_TORCH: the torch that it is compiled against (its version and commit), as tensors lie in memory as that one has them.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+
+#include <initializer_list>
 
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -106,6 +109,19 @@ PyObject* begin(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef methods[] = {STEM_METHOD(values), STEM_METHOD(whole), STEM_METHOD(lines), STEM_METHOD(begin), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
+// Whether the torch that is there is STEM_TORCH.
+bool right_torch() {
+    bool right = false;
+    PyObject *torch = PyImport_ImportModule("torch"), *version = nullptr, *about = nullptr, *commit = nullptr, *here = nullptr;
+    if (torch && (version = PyObject_GetAttrString(torch, "__version__")) && (about = PyObject_GetAttrString(torch, "version")) &&
+        (commit = PyObject_GetAttrString(about, "git_version")) && (here = PyUnicode_FromFormat("%S %S", version, commit))) {
+        right = PyUnicode_CompareWithASCIIString(here, STEM_TORCH) == 0;
+        if (!right) PyErr_Format(PyExc_ImportError, "the checks of tensors are made for torch %s, and this is torch %U", STEM_TORCH, here);
+    }
+    for (PyObject* x : {torch, version, about, commit, here}) Py_XDECREF(x);
+    return right;
+}
+
 }  // namespace
 
-PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__tensors() { return right_torch() ? PyModule_Create(&module) : nullptr; }

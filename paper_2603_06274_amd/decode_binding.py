@@ -8,7 +8,9 @@ Every step runs inside the library's HIP kernels on torch's current stream; ther
 from __future__ import annotations
 
 import ctypes
+import importlib
 import math
+import warnings
 from typing import Optional, Tuple
 
 import torch
@@ -153,9 +155,12 @@ def _lines(t: Optional[torch.Tensor], n: int, each: int, name: str, dev: int, dt
 
 
 try:                                                   # the same three in compiled code, for tensors that are as they have to be
-    from . import _tensors
-except ImportError:                                    # (not built)
+    _tensors = importlib.import_module("._tensors", __package__)
+except ModuleNotFoundError:                            # (not built)
     _tensors = None
+except ImportError as e:
+    _tensors = None
+    warnings.warn("tensors are checked in Python, which takes longer: %s" % e, RuntimeWarning)
 else:
     _tensors.begin(_values, _whole, _lines)
     _values, _whole, _lines = _tensors.values, _tensors.whole, _tensors.lines
