@@ -153,17 +153,15 @@ __device__ __forceinline__ void write_row(const PrefixArgs& a, int token, int he
         a.lse[(int64_t)head * a.tokens + token] = empty ? -__builtin_huge_valf() : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// c times a part's sums, or those of some of its waves.  Where c has become 0 what is finite is gone, and what is not stays: a row's weights are
-// more than 0, however small.  (Of trees, whose sums have only what the row sees that is not finite.)
-template <bool TREE>
-__device__ __forceinline__ f32x4_t carried(f32x4_t o, float c) {
-    f32x4_t y = o * c;
-    if (TREE && c == 0.f) {
+// What is left of sums (of a part, or of some of its waves) whose factor has become 0: what is finite is gone, and what is not stays, as a row's weights
+// are more than 0, however small.  (Of trees, whose sums have only what the row sees that is not finite.)
+__device__ __forceinline__ f32x4_t not_finite(f32x4_t o) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = __builtin_isfinite(o[e]) ? 0.f : o[e];
-    }
-    return y;
+    for (int e = 0; e < 4; ++e) o[e] = __builtin_isfinite(o[e]) ? 0.f : o[e];
+    return o;
 }
+template <bool TREE>
+__device__ __forceinline__ f32x4_t carried(f32x4_t o, float c) { return TREE && c == 0.f ? not_finite(o) : o * c; }
 
 // How the waves of a workgroup share its rows and keys: RW groups of 16 NQ rows times KW groups of 32 keys.  With RW = 1 every wave has
 // keys of its own and waits for no other; with RW > 1 the tile of 32 KW keys in LDS is read by RW waves each, and there are two
@@ -472,9 +470,10 @@ struct Part {
         });
     }
 
-    // The waves' results together -> the rows' outputs, where there are no other parts.  Row m0 of m_end is row m0 of token `first`.
-    template <bool TREE>
-    __device__ __forceinline__ void finish_rows(unsigned char* lds, float2* wave_ml, const PrefixArgs& a, int first, int g, int m0, int m_end) {
+    // The waves' results together -> the rows' outputs, where there are no other parts.  Row m0 of m_end is row m0 of token `first`.  kept: what is
+    // not finite stays, whatever its wave's weight.
+    __device__ __forceinline__ void finish_rows(unsigned char* lds, float2* wave_ml, const PrefixArgs& a, int first, int g, int m0, int m_end,
+                                                bool kept) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -491,8 +490,13 @@ struct Part {
             for (int v = 1; v < KW; ++v) m = fmaxf(m, wave_ml[v * S::kRows + row].x);
             const float mine = __builtin_amdgcn_exp2f(-off[n] - m);
             float* dst = reinterpret_cast<float*>(lds) + (kw * S::kRows + row) * D + 4 * grp;
+            if (__builtin_expect(kept, 0) && mine == 0.f) {
 #pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = carried<TREE>(o[dt][n], mine);
+                for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = not_finite(o[dt][n]);
+                continue;
+            }
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[dt][n] * mine;
         }
         __syncthreads();
         for (int x = threadIdx.x; x < S::kRows * D / 4; x += 64 * kWaves) {
@@ -514,8 +518,7 @@ struct Part {
     }
 
     // The waves' results together -> the part's: rows m0 .. of at most m_end, at `part` (rows of D floats) and ml.
-    template <bool TREE>
-    __device__ __forceinline__ void finish(unsigned char* lds, float2* wave_ml, float* part, float2* ml, int m0, int m_end) {
+    __device__ __forceinline__ void finish(unsigned char* lds, float2* wave_ml, float* part, float2* ml, int m0, int m_end, bool kept) {
         const int lane = threadIdx.x & 63, c16 = lane & 15, grp = lane >> 4, kw = key_group(), row0 = 16 * NQ * row_group();
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
@@ -554,8 +557,13 @@ struct Part {
                 ml[m0 + row] = make_float2(m, sum);
             }
             float* dst = reinterpret_cast<float*>(lds) + (kw * S::kRows + row) * D + 4 * grp;
+            if (__builtin_expect(kept, 0) && mine == 0.f) {
 #pragma unroll
-            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = carried<TREE>(o[dt][n], mine);
+                for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = not_finite(o[dt][n]);
+                continue;
+            }
+#pragma unroll
+            for (int dt = 0; dt < kDT; ++dt) *reinterpret_cast<f32x4_t*>(dst + 16 * dt) = o[dt][n] * mine;
         }
         __syncthreads();
         for (int x = threadIdx.x; x < S::kRows * D / 4; x += 64 * kWaves) {
@@ -615,9 +623,10 @@ __device__ __forceinline__ bool take_out(u32x4_t& values) {
     return any;
 }
 
-// Keys key0 .. key0 + keys - 1 of request r's `len` own, for rows m0 .. of its m_end (new tokens times heads of the group); n new tokens.
+// Keys key0 .. key0 + keys - 1 of request r's `len` own, for rows m0 .. of its m_end (new tokens times heads of the group); n new tokens.  Returns
+// whether there are new tokens' values among them that are not finite (TREE).
 template <typename T, bool TREE, typename S, typename P>
-__device__ __forceinline__ void walk_own(P& t, const PrefixArgs& a, int r, int g, int first, int n, int len, int key0, int keys, int m0,
+__device__ __forceinline__ bool walk_own(P& t, const PrefixArgs& a, int r, int g, int first, int n, int len, int key0, int keys, int m0,
                                          int m_end, unsigned char* lds) {
     const int lane = threadIdx.x & 63;
     const int new0 = len - n - key0;                   // the first new token, among this part's keys
@@ -660,6 +669,7 @@ __device__ __forceinline__ void walk_own(P& t, const PrefixArgs& a, int r, int g
             },
             [&](int tile, int nq, int x) { return tile * S::kKeys + t.key_group() * 32 + x < sees[nq] && (x < 16 ? lo : hi); },
             [](auto&, int) {});
+        return false;
     } else {
         // A value that is not finite times a weight of 0 is NaN: such values of new tokens are taken out of the products, and put into the
         // rows that see them at the end.
@@ -685,7 +695,8 @@ __device__ __forceinline__ void walk_own(P& t, const PrefixArgs& a, int r, int g
                 for (int u = 0; u < P::kPieces * P::kLoads; ++u)
                     if (key + u * P::kRowsPerLoad + lane / P::kChunks >= new0) taken |= take_out<T>(rows[u / P::kLoads][u % P::kLoads]);
             });
-        if (keys <= new0 || !__syncthreads_or(taken) || t.key_group() > 0) return;
+        if (keys <= new0 || !__syncthreads_or(taken)) return false;
+        if (t.key_group() > 0) return true;
         for (int key = max(new0, 0); key < keys; ++key) {
             const int page = page_of(key & ~15), j = key - new0;
             if (page < 0 || (j >> 5) >= a.mask_words) continue;
@@ -702,6 +713,7 @@ __device__ __forceinline__ void walk_own(P& t, const PrefixArgs& a, int r, int g
                     }
             }
         }
+        return true;
     }
 }
 
@@ -725,7 +737,7 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
         const int key0 = split * a.split_keys;
         walk_prefix<SP>(t, a, g, key0, min(a.split_keys, a.prefix_len - key0), lds);
         const int64_t place = ((int64_t)split * a.Hkv + g) * a.rows;
-        t.template finish<TREE>(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows);
+        t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, a.rows, false);
         return;
     }
     // a request's own keys
@@ -753,9 +765,9 @@ __global__ __launch_bounds__(64 * SP::kWaves, D == 256 ? 1 : 2) void prefix_attn
     if (keys <= 0) return;
     PartO t;
     t.load_q(a.q + (int64_t)g * a.G * a.q_sh, a.q_st, a.q_sh, first, a.G, m0, mine);
-    walk_own<T, TREE, SO>(t, a, r, g, first, n, len, key0, keys, m0, mine, lds);
+    const bool kept = walk_own<T, TREE, SO>(t, a, r, g, first, n, len, key0, keys, m0, mine, lds);
     const int64_t place = ((int64_t)(a.prefix_splits + split) * a.Hkv + g) * a.rows + (int64_t)first * a.G;
-    t.template finish<TREE>(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine);
+    t.finish(lds, wave_ml, a.part_o + place * D, a.part_ml + place, m0, mine, kept);
 }
 
 // Small calls in one launch: a workgroup has all keys of a row tile of its request, the prefix's (which are read once per tile then) and its own.
@@ -775,8 +787,8 @@ __global__ __launch_bounds__(64 * S::kWaves) void small_attn_kernel(PrefixArgs a
     if (a.prefix_len > 0) walk_prefix<S>(t, a, g, 0, a.prefix_len, lds);
     const int len = suffix_len(a, r);
     if (S::RW > 1 && a.prefix_len > 0) STEM_LDS_BARRIER();         // no wave is in a tile of the prefix any more
-    if (len > 0) walk_own<T, TREE, S>(t, a, r, g, first, n, len, 0, len, m0, mine, lds);
-    t.template finish_rows<TREE>(lds, wave_ml, a, first, g, m0, mine);
+    const bool kept = len > 0 && walk_own<T, TREE, S>(t, a, r, g, first, n, len, 0, len, m0, mine, lds);
+    t.finish_rows(lds, wave_ml, a, first, g, m0, mine, kept);
 }
 
 // Joins the parts of a row.  D / 4 lanes take four values each, GROUPS such groups of lanes every GROUPS-th part; all that a group reads
@@ -839,19 +851,24 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(PrefixArgs a) {
         for (int x = 0; x < kAtOnce; ++x) top = fmaxf(top, ml[x].x);
         const float then = __builtin_amdgcn_exp2f(m - top);
         l *= then;
-        o = carried<TREE>(o, then);
+        o *= then;
 #pragma unroll
         for (int x = 0; x < kAtOnce; ++x) {
-            const bool there = p0 + x * GROUPS < parts;
-            const float c = there ? __builtin_amdgcn_exp2f(ml[x].x - top) : 0.f;
+            const float c = p0 + x * GROUPS < parts ? __builtin_amdgcn_exp2f(ml[x].x - top) : 0.f;
             l += c * ml[x].y;
-            if constexpr (TREE) {
-                if (there) o += carried<TREE>(part[x], c);
-            } else {
-                if (c != 0.f) o += c * part[x];        // (0 times a part that is not finite is nothing of this row's)
-            }
+            if (TREE || c != 0.f) o += c * part[x];    // (0 times a part that is not finite is nothing of this row's; of trees: see below)
         }
         m = top;
+    }
+    // What is not finite in a tree's part has made NaN of itself where a factor of its was 0: those values once more, by the largest score.
+    if (TREE && __builtin_expect(o[0] != o[0] || o[1] != o[1] || o[2] != o[2] || o[3] != o[3], 0)) {
+        f32x4_t again = {0.f, 0.f, 0.f, 0.f};
+        for (int p = group; p < parts; p += GROUPS) {
+            const int64_t at = p * step + row;
+            again += carried<TREE>(reinterpret_cast<const f32x4_t*>(a.part_o + at * D)[lane], __builtin_amdgcn_exp2f(a.part_ml[at].x - m));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = o[e] != o[e] ? again[e] : o[e];
     }
     if constexpr (GROUPS > 1) {
         group_o[threadIdx.x] = o;
