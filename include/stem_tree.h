@@ -53,8 +53,9 @@ int stem_tree_attn_workspace_bytes(const stem_prefix_shape* shape, size_t* host_
  * bits: a tree's, or none at all), not those up to itself.  Besides:
  *   - max_new is at most STEM_MAX_TREE (STEM_ERR_UNSUPPORTED).  cu_new may not be NULL.  A request's rows from max_new on are left as they were;
  *     new tokens from number 64 * words on are seen by nobody.
- *   - An inf or NaN in a new token's key or value reaches the rows that see it and no others.  (In prefix and earlier tokens: all rows that
- *     see them.)
+ *   - An inf or NaN in a new token's value is in the results of the rows that see it, an infinite one as itself, however small its weight, and in
+ *     no others'; one in its key counts in the scores of the rows that see it, and in no others'.  (In prefix and earlier tokens: in those of all
+ *     rows that see them.)
  */
 int stem_tree_attn(const stem_prefix_shape* shape, const void* q, const void* prefix_k, const void* prefix_v, const void* k_pages,
                    const void* v_pages, const int32_t* table, const int32_t* lens, const int32_t* cu_new, const int64_t* masks,
@@ -86,7 +87,7 @@ int stem_tree_accept_workspace_bytes(const stem_accept_shape* shape, size_t* hos
  *     back that the ring has no room for (1 at least if ring_state is no state).  Unless both are 0 the step is refused: the ring is left
  *     as it is, lens_out and ring_state_out say what was, accepted is 0, path and next_ids -1.
  *   - Entries of path that are no request's are left as they were.
- * workspace: 16-byte aligned, of stem_tree_accept_workspace_bytes, this call's alone until its work has finished.
+ * workspace: 16-byte aligned, of stem_tree_accept_workspace_bytes.  Nothing is written there now, so calls may share one, and any other's.
  * STEM_ERR_UNSUPPORTED if requests * pages_per_request or num_pages * page_size exceeds 2^31 - 1.
  */
 int stem_tree_accept(const stem_accept_shape* shape, const int32_t* parents, const void* draft_ids, const void* target_ids,
