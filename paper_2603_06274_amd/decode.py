@@ -180,7 +180,9 @@ class PagedCache:
         if ids not in self.next_ids:
             raise ValueError("token numbers are int32 or int64")
         tb.need_movable_rows(self.pages)                   # (before the books change)
-        max_new = min(c.max_new, tb.STEM_MAX_TREE) if c.max_new > 0 else tb.STEM_MAX_TREE
+        # (where steps or acceptances are in graphs, the last call's max_new may be another step's)
+        known = c.max_new > 0 and self._step_open is not None and not capturing
+        max_new = min(c.max_new if known else max(self.tokens, 1), tb.STEM_MAX_TREE)
         shape = tb.AcceptShape(c.requests, self.tokens, max_new, c.page_size, c.num_pages, c.pages_per_request)
         tb.stem_tree_accept(shape, parents, draft_ids, target_ids, self.cu_new, self.lens, self.ring_state, self.ring, self.table, self.lens,
                             self.ring_state, self.accepted, self.path, self.next_ids[ids], self.accept_status, self.workspace)

@@ -46,3 +46,25 @@ def test_tried_again():
         made.append((cache.lens, cache.ring_state, cache.ring, cache.table, cache.accepted, cache.path, dec.out))
     for x, y in zip(*made):
         assert torch.equal(x, y)
+
+
+def test_a_replayed_step_of_drafts_behind_an_eager_one_of_single_tokens():
+    R, N, Hkv, d = 3, 7, 2, 64
+    g = torch.Generator().manual_seed(5)
+    prefix = torch.randn(40, Hkv, d, generator=g).to(BF).to(DEV)
+    cache = PagedCache(R, 24, 16, 8, Hkv, d, tokens=R * N)
+    drafts, single = (StemDecode(prefix, prefix.clone(), 4, cache, Rotary(d), max_new=n, tree=True) for n in (N, 1))
+    rows = [torch.randn(R * N, h, d, generator=g).to(BF).to(DEV) for h in (4, Hkv, Hkv)]
+    ones, chain = (torch.tensor(x * R, dtype=torch.int32, device=DEV) for x in ([1], [-1, *range(N - 1)]))
+    new, ids = torch.zeros(R, dtype=torch.int32, device=DEV), torch.zeros(R * N, dtype=torch.int64, device=DEV)
+    drafts.step(*rows, new, parents=chain)             # (of nothing)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        drafts.step(*rows, new, parents=chain)
+    new.fill_(N)
+    for turn in range(3):
+        single.step(*rows, ones)
+        graph.replay()
+        accepted = cache.accept(chain, ids, ids)[0]    # every draft is the model's choice
+        assert cache.accept_refused() == (0, 0) and accepted.tolist() == [N] * R and cache.lens.tolist() == [(turn + 1) * (N + 1)] * R

@@ -64,3 +64,24 @@ def test_a_refused_acceptance_can_be_tried_again(calls):
         assert cache.accept_refused() == (0, 0)
         with pytest.raises(RuntimeError):
             cache.accept(x, x, x)
+
+
+def test_replayed_steps_may_have_more_new_tokens_than_the_last_call(calls, monkeypatch):
+    """Where steps or acceptances are in graphs, an acceptance is of whichever step has been replayed: of as many tokens as there are rows."""
+    asked = []
+    monkeypatch.setattr(tb, "stem_tree_accept", lambda shape, *a: asked.append(shape.c[torch.int32].max_new))
+    x = whole(4)
+    for captured in ("step", "accept", None):
+        cache = PagedCache(2, 4, 16, 2, 1, 64, tokens=4, device="cpu")
+        cache._capturing = lambda: captured == "step"
+        cache.advance(None, 3)
+        cache._capturing = lambda: False
+        cache.advance(None, 1)
+        cache._capturing = lambda: captured == "accept"
+        cache.accept(x, x, x)
+    cache.advance()                                # any number of new tokens
+    cache.accept(x, x, x)
+    large = PagedCache(2, 200, 16, 100, 1, 64, tokens=2000, device="cpu")
+    large.advance()
+    large.accept(*[whole(2000)] * 3)
+    assert asked == [4, 4, 1, 4, tb.STEM_MAX_TREE]
